@@ -341,6 +341,117 @@ fq_status_t fq_fused_host_io_async(const fq_layout_t* L, const void* X_host, uin
                                    const void* packed_outliers, void* y_dev, void* Y_host,
                                    void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* ------------------------------------------------------- microscaled FP4 operators
+ *
+ * Matrices whose values are e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) under a scale for each block of
+ * consecutive values of a row, in the two forms that the tensor cores multiply as they are:
+ *   FQ_MXFP4   blocks of 32, scale a power of two (E8M0 byte: 2^(b - 127), 255 = NaN)
+ *   FQ_NVFP4   blocks of 16, scale an E4M3 number (sign bit 0, 0x7f = NaN) times one FP32 scale of the tensor
+ *
+ * Quantising a block with the largest magnitude `amax`:
+ *   FQ_MXFP4   d = 2^e, e = max(floor(log2 amax) - 2, -127)
+ *   FQ_NVFP4   s = E4M3(amax / (6 ts)), the quotient in binary64, rounded to nearest even, at most 448, at least 2^-9 if
+ *              amax > 0; d = s ts rounded to binary32
+ *   code       e2m1(x / d) of the exact quotient, rounded to nearest even, at most 6 in magnitude
+ * A block that holds a NaN or an infinity gets the scale NaN and codes 0: it reads back as NaN.  A tensor scale that is
+ * not in [2^-100, 2^100] gives NaN scales throughout.
+ *
+ * Stored form of a rows x K matrix (K a multiple of 32):
+ *   codes    rows x K/2 bytes, row-major, value k in nibble k % 2 of byte k / 2 (even k: low nibble)
+ *   scales   atoms of 512 bytes, each 128 rows by 4 blocks: the scale of row r and block b is byte
+ *                (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4
+ *            of atom (r / 128) * ceil(blocks / 4) + b / 4.  Blocks beyond K inside the last atom of a row are 0; bytes of rows
+ *            beyond the last are neither read nor written.
+ * (The scales are then in the order in which they go to tensor memory: an atom is one 32x128b copy.)
+ *
+ * All calls take any number of rows from 1, enqueue on the stream and return.  Unlike the weights of the fused INT4 call,
+ * every array may be written by a kernel that is still running in the stream when the call is made: each kernel
+ * here waits for the grid before it before it reads or writes anything.
+ * Outputs must not overlap inputs or each other (FQ_ERR_INVALID_ARG), except where it is said.
+ */
+#define FQ_MXFP4 0u
+#define FQ_NVFP4 1u
+#define FQ_TYPE_BF16 0u
+#define FQ_TYPE_FP16 1u
+#define FQ_TYPE_FP32 2u
+#define FQ_MX_MAX_K (1u << 20)
+#define FQ_MX_MAX_ROWS ((1u << 31) - 256u)
+#define FQ_NORM_MAX_D 16384u
+
+typedef struct fq_mx_layout {
+    uint32_t abi;     /* FQ_ABI_VERSION */
+    uint32_t rows, K;
+    uint32_t format;  /* FQ_MXFP4 or FQ_NVFP4 */
+} fq_mx_layout_t;
+
+/* Errors: FQ_ERR_INVALID_ARG for an unknown format or no rows, FQ_ERR_UNSUPPORTED_SHAPE for K that is 0, no multiple of
+ * 32 or above FQ_MX_MAX_K, and for more than FQ_MX_MAX_ROWS rows. */
+fq_status_t fq_mx_get_layout(uint32_t rows, uint32_t K, uint32_t format, fq_mx_layout_t* out);
+fq_status_t fq_mx_sizes(const fq_mx_layout_t* L, size_t* code_bytes, size_t* scale_bytes);
+
+/* X: device, rows x K of `type`, row stride ldx elements (any that is at least K; rows on 16-byte boundaries are read faster).
+ * tensor_scale: device, one FP32 (FQ_NVFP4; null means 1), null for FQ_MXFP4.  codes, scales: device, 16-byte aligned. */
+fq_status_t fq_mx_quantize(const fq_mx_layout_t* L, const void* X, uint32_t type, uint64_t ldx, const float* tensor_scale,
+                           void* codes, void* scales, void* cuda_stream);
+
+/* The gated product of a decoder's MLP, quantised: h = gate / (1 + exp(-gate)) * up, rounded once to `type` (FQ_TYPE_BF16 or
+ * FQ_TYPE_FP16), then as fq_mx_quantize.  gate, up: device, rows x K, row strides ld_gate and ld_up (the halves of one
+ * rows x 2K array, for instance). */
+fq_status_t fq_mx_quantize_swiglu(const fq_mx_layout_t* L, const void* gate, uint64_t ld_gate, const void* up, uint64_t ld_up,
+                                  uint32_t type, const float* tensor_scale, void* codes, void* scales, void* cuda_stream);
+
+/* The values that codes and scales stand for, code * d (d as above, in binary32), rounded once to `type`.  Y: device, rows x K, row
+ * stride ldy. */
+fq_status_t fq_mx_dequantize(const fq_mx_layout_t* L, const void* codes, const void* scales, const float* tensor_scale, void* Y,
+                             uint32_t type, uint64_t ldy, void* cuda_stream);
+
+/*
+ * What stands between two blocks of a decoder: the norm after a block with its gate and residual scale, the residual
+ * sum, the norm before the next block, and the quantisation of its result.  Per row of D values:
+ *     y = block                                              (without block_weight)
+ *     y = block * rsqrt(mean(block^2) + eps) * block_weight  (with it)
+ *     r = X + residual_scale * gate * y                      (r = X without block; gate 1 without gate)
+ *     h = r * rsqrt(mean(r^2) + eps) * weight                (weight 1 without weight)
+ * r and h are each rounded once (h is computed from the unrounded r), codes and scales are those that fq_mx_quantize makes
+ * of the rounded h.  Sums run in binary64, and a result too near a rounding border for binary32 is settled in binary64.
+ * Any of R, H and (codes, scales) may be null, not all.  All of `type`, FQ_TYPE_BF16 or FQ_TYPE_FP16; vectors of D on any
+ * boundary; D from 1 to FQ_NORM_MAX_D; with codes, layout.rows = rows and layout.K = D.
+ * R or H may be X or block themselves (same address and row stride): the sum in place.
+ */
+typedef struct fq_norm_args {
+    uint32_t rows, D, type;
+    float eps, residual_scale;
+    const void* X;            /* rows x D, the residual stream */
+    uint64_t ld_x;
+    const void* block;        /* rows x D or null: what the block before put out */
+    uint64_t ld_block;
+    const void* block_weight; /* D or null */
+    const void* gate;         /* rows x D, or one row for all (ld_gate 0), or null */
+    uint64_t ld_gate;
+    const void* weight;       /* D or null */
+    void* R;                  /* rows x D or null */
+    uint64_t ld_r;
+    void* H;                  /* rows x D or null */
+    uint64_t ld_h;
+    const fq_mx_layout_t* layout; /* with codes and scales, or null */
+    const float* tensor_scale;
+    void* codes;
+    void* scales;
+} fq_norm_args_t;
+fq_status_t fq_norm_block(const fq_norm_args_t* a, void* cuda_stream);
+
+/*
+ * Product of two quantised matrices, Y[m, n] = ts_x ts_w sum_k x[m, k] w[n, k]: x has LX->rows rows (tokens), w LW->rows
+ * rows (output features, K contiguous: a linear layer's weight as it is usually kept).  Same K and format.  Sums in FP32
+ * on the tensor cores (tcgen05.mma block_scale), one rounding to `type`.  Y: device, row stride ldy >= LW->rows.
+ * A split along K is added in a fixed order, so results are run-to-run reproducible.  workspace: FQ_MX_WORKSPACE_BYTES of
+ * device memory, zeroed once, for fq_check_status; calls may share it.
+ */
+#define FQ_MX_WORKSPACE_BYTES 33024u
+fq_status_t fq_mx_gemm(const fq_mx_layout_t* LX, const void* x_codes, const void* x_scales, const float* x_tensor_scale,
+                       const fq_mx_layout_t* LW, const void* w_codes, const void* w_scales, const float* w_tensor_scale, void* Y,
+                       uint32_t type, uint64_t ldy, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* Synchronise the stream and return the scratch's status word: FQ_OK,
  * FQ_ERR_TIMEOUT if a bounded wait expired in a kernel, or FQ_ERR_FORMAT if a
  * kernel found bucket descriptors that point outside the packets staged for

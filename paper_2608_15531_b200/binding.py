@@ -25,6 +25,9 @@ FQ_ERR_FORMAT = -6
 FQ_MAX_M = 128
 FQ_VALUE_BF16 = 0
 FQ_VALUE_FP16 = 1
+FQ_MXFP4 = 0
+FQ_NVFP4 = 1
+FQ_MX_WORKSPACE_BYTES = 33024
 
 EXPORTS = [
     "fq_get_layout", "fq_pack_int4_sizes", "fq_pack_int4", "fq_unpack_int4", "fq_encode_tilecoo_sizes",
@@ -32,6 +35,7 @@ EXPORTS = [
     "fq_repurpose_pad_slots",
     "fq_fused_w4a16_outlier_gemm", "fq_fused_w4a16_outlier_gemm_noalloc", "fq_unfused_gemm", "fq_unfused_spmm", "fq_fused_host_io",
     "fq_fused_host_io_async",
+    "fq_mx_get_layout", "fq_mx_sizes", "fq_mx_quantize", "fq_mx_quantize_swiglu", "fq_mx_dequantize", "fq_mx_gemm", "fq_norm_block",
     "fq_check_status", "fq_last_error",
 ]
 
@@ -41,6 +45,11 @@ class Layout(ctypes.Structure):
                  ("abi", "K", "N", "group", "BK", "BN", "buckets_per_tile", "wq_interleave", "coo_unit_bytes",
                   "max_tile_packets", "max_bucket_packets", "max_tail_packets", "tilecoo_encoded", "kernel_hint",
                   "slot_order", "value_type")])
+
+
+class MxLayout(ctypes.Structure):
+    """A microscaled FP4 matrix of rows x K values: ``format`` is FQ_MXFP4 or FQ_NVFP4."""
+    _fields_ = [(n, ctypes.c_uint32) for n in ("abi", "rows", "K", "format")]
 
 
 class FqError(RuntimeError):
@@ -69,7 +78,7 @@ _call = None
 
 
 def _pycall():
-    """The CPython entry to the fused calls (``_fqcall.so``), which passes tensors on without ctypes."""
+    """The CPython entry to the device calls (``_fqcall.so``), which passes tensors on without ctypes."""
     global _call
     if _call is None:
         lib()
@@ -267,3 +276,54 @@ def fq_check_status(workspace, stream=None) -> None:
 
 def fq_last_error() -> str:
     return lib().fq_last_error().decode(errors="replace")
+
+
+# ------------------------------------------------------------------ microscaled FP4
+#
+# X, Y, gate, ...: CUDA tensors of bfloat16, float16 or (quantize, dequantize, the product's Y) float32, two-dimensional, columns adjacent,
+# any row stride.  codes, scales: contiguous CUDA tensors of at least fq_mx_sizes(L) bytes.  tensor_scale: one float32
+# value on the device (FQ_NVFP4; None means 1).  All on one device, which need not be the current one; the stream is the
+# given one or that device's current stream.
+
+def fq_mx_get_layout(rows: int, K: int, format: int) -> MxLayout:
+    L = MxLayout()
+    if not (0 <= rows < 2 ** 32 and 0 <= K < 2 ** 32 and 0 <= format < 2 ** 32):
+        raise FqError(FQ_ERR_INVALID_ARG, f"rows = {rows}, K = {K}, format = {format}")
+    _check(lib().fq_mx_get_layout(ctypes.c_uint32(rows), ctypes.c_uint32(K), ctypes.c_uint32(format), ctypes.byref(L)))
+    return L
+
+
+def fq_mx_sizes(L: MxLayout):
+    """(bytes of the codes, bytes of the scales)"""
+    a, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(lib().fq_mx_sizes(ctypes.byref(L), ctypes.byref(a), ctypes.byref(b)))
+    return a.value, b.value
+
+
+def fq_mx_quantize(L: MxLayout, X, codes, scales, tensor_scale=None, stream=None) -> None:
+    """Rows of values to codes and block scales."""
+    _check((_call or _pycall()).mx_quantize(L, X, codes, scales, tensor_scale, stream))
+
+
+def fq_mx_quantize_swiglu(L: MxLayout, gate, up, codes, scales, tensor_scale=None, stream=None) -> None:
+    """gate / (1 + exp(-gate)) * up, rounded to the inputs' type, to codes and block scales."""
+    _check((_call or _pycall()).mx_quantize_swiglu(L, gate, up, codes, scales, tensor_scale, stream))
+
+
+def fq_mx_dequantize(L: MxLayout, codes, scales, Y, tensor_scale=None, stream=None) -> None:
+    """The values that codes and scales stand for, in Y's type."""
+    _check((_call or _pycall()).mx_dequantize(L, codes, scales, Y, tensor_scale, stream))
+
+
+def fq_mx_gemm(LX: MxLayout, x_codes, x_scales, LW: MxLayout, w_codes, w_scales, Y, workspace, x_tensor_scale=None,
+               w_tensor_scale=None, stream=None) -> None:
+    """Y (LX.rows x LW.rows) = x times w transposed.  workspace: FQ_MX_WORKSPACE_BYTES, zeroed once; fq_check_status reads it."""
+    _check((_call or _pycall()).mx_gemm(LX, x_codes, x_scales, x_tensor_scale, LW, w_codes, w_scales, w_tensor_scale, Y, workspace, stream))
+
+
+def fq_norm_block(X, eps: float, *, block=None, block_weight=None, gate=None, residual_scale: float = 1.0, R=None, weight=None,
+                  H=None, layout: MxLayout | None = None, codes=None, scales=None, tensor_scale=None, stream=None) -> None:
+    """What stands between two blocks: R = X + residual_scale * gate * norm(block) (norm only with block_weight), H = norm(R) * weight,
+    and H quantised (layout, codes, scales).  gate: as X, or one row for all rows.  R or H may be X or block (in place)."""
+    _check((_call or _pycall()).norm_block(X, eps, block, block_weight, gate, residual_scale, R, weight, H, layout, codes, scales,
+                                           tensor_scale, stream))

@@ -10,12 +10,13 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfq.so")
-SOURCES = [os.path.join(CSRC, "fq_host.cpp"), os.path.join(CSRC, "fq_kernels.cu")]
-HEADERS = [os.path.join(CSRC, "fq_internal.h"), os.path.join(CSRC, "fq_shares.h"), os.path.join(CSRC, "fq_tc_kernel.cuh"), os.path.join(CSRC, "fq_mma_kernel.cuh"),
+SOURCES = [os.path.join(CSRC, "fq_host.cpp"), os.path.join(CSRC, "fq_kernels.cu"), os.path.join(CSRC, "fq_mx_kernels.cu")]
+HEADERS = [os.path.join(CSRC, "fq_internal.h"), os.path.join(CSRC, "fq_launch.h"), os.path.join(CSRC, "fq_ptx.cuh"), os.path.join(CSRC, "fq_mx.cuh"),
+           os.path.join(CSRC, "fq_mx_gemm_kernel.cuh"), os.path.join(CSRC, "fq_shares.h"), os.path.join(CSRC, "fq_tc_kernel.cuh"), os.path.join(CSRC, "fq_mma_kernel.cuh"),
            os.path.join(CSRC, "fq_direct_kernel.cuh"), os.path.join(ROOT, "include", "fq.h")]
 
 NVCC_FLAGS = [
-    "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+    "-gencode", "arch=compute_100a,code=sm_100a", "--threads", "4", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC,-fopenmp,-ffp-contract=off,-fno-fast-math", "-shared",
     "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]

@@ -23,145 +23,17 @@
 #include <mutex>
 
 #include "fq_internal.h"
+#include "fq_launch.h"
+#include "fq_ptx.cuh"
 #include "fq_shares.h"
 
 namespace cg = cooperative_groups;
 namespace fq {
 
 constexpr int kBK = 128;
-constexpr int kSmemBudget = 232448;    // 227 KB per CTA on sm_100
-constexpr uint32_t kSmemOneCta = 116736;   // of which no two CTAs fit on an SM: 228 KB, and 1 KB of a CTA is the system's
-constexpr unsigned long long kWaitLimitNs = 2000000000ull;
 constexpr uint32_t kTmemCols = 512;
 
 
-// ----------------------------------------------------------------------------- PTX helpers
-
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
-}
-// A release, like every arrival here: also that of a consumer, whose reads of a stage come before the copy that fills it next,
-// and that of a warp which has waited for a copy and tells the next warp so.
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-    asm volatile("{\n .reg .b64 st;\n mbarrier.arrive.shared::cta.b64 st, [%0];\n}" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive_expect_tx(uint32_t bar, uint32_t bytes) {
-    asm volatile("{\n .reg .b64 st;\n mbarrier.arrive.expect_tx.shared::cta.b64 st, [%0], %1;\n}" ::"r"(bar), "r"(bytes)
-                 : "memory");
-}
-// more bytes for the barrier's current phase, without arriving
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-// A waiting thread sleeps in hardware for a while instead of spinning on the issue slots that the working warps of the
-// CTA need.  No suspend-time hint: with one of 20 us the waits of the tcgen05 kernel returned later (8192 x 28672 at
-// 32 rows 80.4 us, without it 78.0; spinning on test_wait instead 83.1).
-__device__ __forceinline__ uint32_t mbar_try_wait(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok;
-}
-__device__ __forceinline__ uint32_t mbar_test_wait(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok;
-}
-__device__ __forceinline__ unsigned long long globaltimer_ns() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-// Bounded wait, slow part.  Inlined: a call in the pipeline loops constrains the register allocation of
-// the code around it (measured: 3 % on the dense-only kernel).
-__device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* status) {
-    uint32_t spins = 0;
-    unsigned long long t0 = 0;
-    while (!mbar_try_wait(bar, parity)) {
-        if ((++spins & 0xf) == 0) {
-            if (*abort_flag) return false;
-            unsigned long long now = globaltimer_ns();
-            if (t0 == 0) {
-                t0 = now;
-            } else if (now - t0 > kWaitLimitNs) {
-                *abort_flag = 1;
-                atomicExch(status, (uint32_t)FQ_ERR_TIMEOUT);
-                return false;
-            }
-        }
-    }
-    return true;
-}
-// Bounded wait: false if this CTA is giving up (its own limit expired, or another warp's did).
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag,
-                                          uint32_t* status) {
-    if (mbar_test_wait(bar, parity)) return true;   // already complete
-    return mbar_wait_slow(bar, parity, abort_flag, status);
-}
-// Warp-uniform form: every lane waits, and the warp gives up together.  Every lane polls and the outcome is a vote, which
-// the compiler knows to be the same in every lane; with one lane polling and a shuffle the loops around the waits were
-// compiled as divergent (streaming kernel 5 to 7 % slower: 4096 x 28672 at one row 23.5 us, so 22.3).
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* status) {
-    const bool ok = mbar_wait(bar, parity, abort_flag, status);
-    return __all_sync(0xffffffffu, ok);
-}
-// A wait of a CTA that is leaving: no status, no abort flag, at most 100 ms (and no fewer than 4096 polls: the clock also runs while
-// the context is switched out).
-__device__ __forceinline__ void mbar_wait_leaving(uint32_t bar, uint32_t parity) {
-    const unsigned long long t0 = globaltimer_ns();
-    for (uint32_t polls = 0; !mbar_try_wait(bar, parity); ++polls)
-        if (polls >= 4096 && globaltimer_ns() - t0 > 100000000ull) return;
-}
-// What a producer does that gives up: it lets the copies already issued land before the CTA's shared memory goes away.
-__device__ __forceinline__ void let_copies_land(uint32_t bar_full, uint32_t issued, uint32_t S) {
-    for (uint32_t j = (issued > S ? issued - S : 0); j < issued; ++j) mbar_wait_leaving(bar_full + 8 * (j % S), (j / S) & 1);
-}
-__device__ __forceinline__ void bulk_g2s(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-                 "l"(src), "r"(bytes), "r"(bar)
-                 : "memory");
-}
-// (w & 0x000f000f) | 0x43004300: two codes -> two BF16 values 128 + q
-__device__ __forceinline__ uint32_t codes_to_bf16x2(uint32_t w) {
-    uint32_t r;
-    asm("lop3.b32 %0, %1, 0x000f000f, 0x43004300, 0xea;" : "=r"(r) : "r"(w));
-    return r;
-}
-__device__ __forceinline__ float bf16lo(uint32_t v) { return __uint_as_float(v << 16); }
-__device__ __forceinline__ float bf16hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
-__device__ __forceinline__ float bf16_bits_to_float(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
-__device__ __forceinline__ uint16_t float_to_bf16_bits(float f) {
-    return __bfloat16_as_ushort(__float2bfloat16_rn(f));
-}
-__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3)
-                 : "r"(addr));
-}
-
-// ---- tcgen05 / tensor memory
-__device__ __forceinline__ void tmem_alloc(uint32_t smem_dst, uint32_t ncols) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(ncols) : "memory");
-}
-__device__ __forceinline__ void tmem_relinquish() {
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 // Walks a CTA's units without integer division: ring slot s with its parity, tile tn, k-step kt.
 struct UnitIter {
     uint32_t u, it, s, ph, tn, kt;
@@ -346,21 +218,6 @@ __global__ void __launch_bounds__(kSpmmThreads, 2) fq_spmm_kernel(const uint16_t
 
 // ----------------------------------------------------------------------------- launch plumbing
 
-static inline uint32_t round_up(uint32_t v, uint32_t a) { return (v + a - 1) / a * a; }
-
-static int sm_count_cached() {
-    static int cached[64];
-    static std::once_flag once;
-    std::call_once(once, [] { std::memset(cached, 0, sizeof(cached)); });
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return -1;
-    if (cached[dev] == 0) {
-        int n = 0;
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return -1;
-        cached[dev] = n;
-    }
-    return cached[dev];
-}
 
 // The tcgen05 kernel's variant for a launch: the batch rows its tensor memory and drain warps are laid out for.
 static inline uint32_t tc_rows(uint32_t m) { return m <= 16 ? 16u : (m <= 32 ? 32u : (m <= 64 ? 64u : 128u)); }
@@ -421,14 +278,7 @@ static fq_status_t make_plan_tc(const fq_layout_t* L, uint32_t M, TcPlan& pl) {
 // The tiled tensor map of a launch's activations: boxes of 64 K values by the MMA's batch rows, 128-byte swizzle;
 // rows beyond M read as zero.
 static fq_status_t encode_x_map(const fq_layout_t* L, const uint16_t* X, uint32_t M, uint32_t nmma, CUtensorMap* map) {
-    typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static const EncodeFn fn = [] {
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult qr;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &qr) != cudaSuccess || qr != cudaDriverEntryPointSuccess) f = nullptr;
-        return (EncodeFn)f;
-    }();
+    const EncodeFn fn = tensor_map_encoder();
     if (!fn) return fail(FQ_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
     const cuuint64_t dims[2] = {L->K, M}, strides[1] = {(cuuint64_t)L->K * 2};
     const cuuint32_t box[2] = {64, nmma}, ones[2] = {1, 1};
@@ -656,25 +506,6 @@ static TcKernelFn pick_tc_kernel(uint32_t nr, uint32_t g, bool coop) {          
     if (nr == 64) return coop ? pick_tc_group<64, true>(g) : pick_tc_group<64, false>(g);
     return nr == 32 ? pick_tc_group<32, true>(g) : pick_tc_group<16, true>(g);
 }
-
-// cudaFuncSetAttribute costs several microseconds: do it once per (kernel, device).
-static cudaError_t ensure_smem_attr(const void* fn, int bytes) {
-    struct Seen { const void* fn; int dev; };
-    static Seen seen[256];
-    static int nseen = 0;
-    static std::mutex mu;
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    std::lock_guard<std::mutex> lock(mu);
-    for (int i = 0; i < nseen; ++i)
-        if (seen[i].fn == fn && seen[i].dev == dev) return cudaSuccess;
-    e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == cudaSuccess && nseen < 256) seen[nseen++] = Seen{fn, dev};
-    return e;
-}
-
-static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 // Argument checks of the device entry points: nothing is enqueued when one fails.
 static fq_status_t check_gemm_args(const fq_layout_t* L, const void* X, uint32_t M, const void* wq, const void* scale,

@@ -41,12 +41,6 @@
 // Before, launches of 17 to 32 rows ran on the 8-bit integer tensor path, activations as three limbs and outliers applied row
 // by row (8192 x 28672 at 32 rows 124.5 us; 4096 x 28672 at 128 rows, in four launches, 305, now 53).
 
-__device__ __forceinline__ bool elect_one() {
-    uint32_t e;
-    asm volatile("{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n selp.u32 %0, 1, 0, e;\n}" : "=r"(e));
-    return e != 0;
-}
-
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
@@ -54,28 +48,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-// 16 or 32 consecutive 32-bit cells of this thread's tensor-memory lane
-template <int N>
-__device__ __forceinline__ void tmem_ld(uint32_t taddr, float (&r)[N]) {
-    if constexpr (N == 16) {
-        asm volatile(
-            "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-            : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
-              "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
-            : "r"(taddr) : "memory");
-    } else {
-        static_assert(N == 32, "unsupported tcgen05.ld width");
-        asm volatile(
-            "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-            "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-            : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]),
-              "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]),
-              "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]),
-              "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
-            : "r"(taddr) : "memory");
-    }
-}
-
 // The eight MMAs of a unit, D[128 x N] (+)= A[128 x 16] * B[16 x N] for each 16 of its 128 k, BF16 in, FP32 out, and the
 // commits that follow them.  Whole warp, converged, with warp-uniform operands; one elected lane issues.  One asm block, so
 // that the address arithmetic is not in a divergent branch: there the operands of each MMA have to be moved into
@@ -161,22 +133,6 @@ __device__ __forceinline__ void umma_outliers(uint32_t d, uint32_t a, uint32_t a
         " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%8];\n}"
         ::"r"(d), "r"(a), "r"(b0), "r"(b1), "r"(b_hi), "r"(idesc), "r"(acc), "r"(a_hi), "r"(bar0)
         : "memory");
-}
-__device__ __forceinline__ void umma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-// K-major operands.  No swizzle (the outlier tile): core matrices of 8 rows x 16 bytes, `lbo` bytes from one 16-byte
-// column of K to the next, 128 bytes from one group of eight rows to the next.
-__device__ __forceinline__ uint64_t desc_plain(uint32_t saddr, uint32_t lbo) {
-    return (uint64_t)((saddr & 0x3ffffu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
-}
-// 128-byte swizzle (the activations): rows of 64 K values, 1024 bytes from one group of eight rows to the next.
-__device__ __forceinline__ uint64_t desc_sw128(uint32_t saddr) {
-    return (uint64_t)((saddr & 0x3ffffu) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t x, uint32_t y, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 __device__ __forceinline__ uint32_t add_bf16x2(uint32_t a, uint32_t b) {
     uint32_t r;
