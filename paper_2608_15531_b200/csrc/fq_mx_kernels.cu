@@ -26,8 +26,10 @@ __device__ __forceinline__ void grid_start() {
 
 // ------------------------------------------------------------------------------------ quantising and reading back
 
-// A warp takes 256 consecutive values of four rows that are 32 apart, whose scales share the 16-byte lines of an atom:
-// eight values of each row to a lane, four loads in flight.
+// A warp takes 512 consecutive values, 16 to a lane (32 bytes of a 16-bit type: one load), of G rows that are 32 apart.  With
+// G = 4 (two for gated products: registers) their scales share the 16-byte lines of an atom, and four loads are in flight; with
+// G = 1 a small matrix is spread over more warps.  16 values are a block of FQ_NVFP4, whose scale (a quotient and its rounding) is then
+// computed by one lane.
 struct MxParams {
     const void* a;               // X, or the gate
     const void* b;               // up
@@ -36,114 +38,180 @@ struct MxParams {
     uint32_t* codes;
     uint8_t* scales;
     void* y;                     // (reading back)
-    uint32_t rows, K, atoms, chunks;      // chunks of 256 values
+    uint32_t rows, K, atoms, chunks;      // chunks of 512 values
     uint64_t tasks;
+    int lie;                     // RowsLie
 };
+template <int G>
 struct MxTask {
-    uint32_t row0, k;            // the first of the four rows, this lane's first value
+    uint32_t row0, k;            // the first of the rows, this lane's first value
     bool any;
     __device__ __forceinline__ explicit MxTask(const MxParams& p) {
         const uint64_t w = (uint64_t)blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32;
-        const uint64_t line = w / p.chunks;                               // row inside a tile, and the tile
+        uint64_t line;
+        if ((p.tasks >> 32) == 0) line = (uint32_t)w / p.chunks;
+        else line = w / p.chunks;
         any = w < p.tasks;
-        row0 = (uint32_t)(line >> 5) * 128 + (uint32_t)(line & 31);
-        k = (uint32_t)(w - line * p.chunks) * 256 + (threadIdx.x & 31) * 8;
+        row0 = G == 1 ? (uint32_t)line : (uint32_t)(line >> 5) * (32 * G) + (uint32_t)(line & 31);
+        k = (uint32_t)(w - line * p.chunks) * 512 + (threadIdx.x & 31) * 16;
     }
 };
 constexpr int kMxThreads = 256;
 
-template <class T, bool VEC>
-__device__ __forceinline__ void gated8(const T* gate, const T* up, float (&h)[8]) {
-    float g[8], u[8];
-    load8<T, VEC>(gate, 8, g);
-    load8<T, VEC>(up, 8, u);
+// gate / (1 + exp(-gate)) * up in binary32.  exp(-g) is 2^t (1 + c), where t is -g log2(e) as rounded and c = -g - t ln(2), what the
+// rounding left (below 2^-17).  Off by at most 2^-22 (ex2) + 2^-23 (rcp) and four roundings, 5 * 2^-23 of the result, as
+// long as the gate is not below -80, where 1 + exp(-g) may leave binary32.
+__device__ __forceinline__ float gated(float g, float u) {
+    constexpr float L = 1.44269504f, N = 0.693147181f, N2 = -1.90465421e-9f;      // log2(e); ln(2) and what binary32 leaves of it
+    const float t = -L * g, c = fmaf(-N2, t, fmaf(-N, t, -g));
+    float e, s;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+    e = fmaf(e, c, e) + 1.0f;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(e));
+    return g * s * u;
+}
+__device__ __noinline__ float gated_exact(float g, float u) { return (float)((double)g / (1.0 + exp(-(double)g)) * (double)u); }
+
+// A lane's 16 gated products, rounded to T and quantised.  The exact product lies between the computed one a little less and a little
+// more; where both round alike that is the result.  Where some do not (1 in 8192 values of BF16, 1 in 1024 of FP16), but
+// give the same codes and scales, no matter (h itself is not put out); else (one in some thousand warps) the warp takes what
+// is in question in binary64.
+template <class T, bool NV>
+__device__ __forceinline__ void quantize_gated16(const Words8& gate, const Words8& up, const TensorScale& ts, uint2& codes, uint32_t& scale) {
+    constexpr float E = 0x1p-20f;
+    Words8 lo, hi;
+    uint32_t differ = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        float f = (g[i] / (1.0f + expf(-g[i]))) * u[i];
-        // 1 + exp(-g) beyond -60 loses what the product may still hold
-        if ((near_border(f, T()) && g[i] != 0.0f && u[i] != 0.0f) || g[i] < -60.0f) f = (float)((double)g[i] / (1.0 + exp(-(double)g[i])) * (double)u[i]);
-        h[i] = to_float(from_float<T>(f));
+        const float2 g = unpack2(gate.w[i], T()), u = unpack2(up.w[i], T());
+        const float a = gated(g.x, u.x), b = gated(g.y, u.y);
+        lo.w[i] = pack2(fmaf(a, -E, a), fmaf(b, -E, b), T());
+        hi.w[i] = pack2(fmaf(a, E, a), fmaf(b, E, b), T());
+        differ |= lo.w[i] ^ hi.w[i];
+    }
+    // the gate's bits as an unsigned number are above those of -80 where it is below -80 (or a NaN with a sign)
+    constexpr uint32_t deep = sizeof(T) == 2 && Border<T>::SHIFT ? 0xd500u : 0xc2a0u;
+    const uint4 g0 = gate.half(0), g1 = gate.half(1);
+    const uint32_t gm = max_u16x2(max_u16x2(max_u16x2(g0.x, g0.y), max_u16x2(g0.z, g0.w)), max_u16x2(max_u16x2(g1.x, g1.y), max_u16x2(g1.z, g1.w)));
+    quantize16<NV, T>(hi, ts, codes, scale);
+    // products so small that binary32 may have lost bits on the way: only where a whole block is
+    const uint32_t m = max_u16x2(max_magnitude(hi.half(0)), max_magnitude(hi.half(1)));
+    bool redo = max(gm & 0xffffu, gm >> 16) > deep || (!Border<T>::SHIFT && max(m & 0xffffu, m >> 16) < 0x1780u && m);
+    if (__any_sync(0xffffffffu, differ != 0 || redo)) {
+        uint2 other;
+        uint32_t other_scale;
+        quantize16<NV, T>(lo, ts, other, other_scale);
+        if (__any_sync(0xffffffffu, redo || other.x != codes.x || other.y != codes.y || other_scale != scale)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t ask = redo ? 0xffffffffu : lo.w[i] ^ hi.w[i];
+                const float2 g = unpack2(gate.w[i], T()), u = unpack2(up.w[i], T());
+                if (ask & 0xffffu) hi.w[i] = (hi.w[i] & 0xffff0000u) | pack2(gated_exact(g.x, u.x), 0.0f, T());
+                if (ask >> 16) hi.w[i] = (hi.w[i] & 0xffffu) | pack2(0.0f, gated_exact(g.y, u.y), T());
+            }
+            quantize16<NV, T>(hi, ts, codes, scale);
+        }
     }
 }
 
-template <class T, bool NV, bool GATED, bool VEC>
+template <class T, bool NV, bool GATED, int G>
 __global__ void __launch_bounds__(kMxThreads) fq_mx_quantize_kernel(const MxParams p) {
-    const MxTask task(p);
+    const MxTask<G> task(p);
     grid_start();
     if (!task.any) return;
     TensorScale ts;
     if constexpr (NV) ts.read(p.ts);
-    const uint32_t lane = threadIdx.x & 31, k = task.k;
-    constexpr int AL = Mx<NV>::ATOM_LANES;
-    float v[4][8];
+    const uint32_t k = task.k;
+    constexpr bool F32 = sizeof(T) == 4, TWO = F32 || GATED;
+    Words8 in[G], in2[TWO ? G : 1];                        // the second: values 8 to 15 of FP32, or up
+    const bool inside = k < p.K;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
+    for (int g = 0; g < G; ++g) {
         const uint32_t r = task.row0 + 32 * g;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[g][i] = 0.0f;
-        if (r < p.rows && k < p.K) {
+        if (inside && r < p.rows) {
             const T* a = (const T*)p.a + (uint64_t)r * p.ld_a + k;
-            if constexpr (GATED) gated8<T, VEC>(a, (const T*)p.b + (uint64_t)r * p.ld_b + k, v[g]);
-            else load8<T, VEC>(a, 8, v[g]);
-        }
-    }
-    uint32_t words[4];
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        const uint32_t r = task.row0 + 32 * g;
-        uint32_t codes, scale;
-        quantize8<NV>(v[g], ts, codes, scale);
-        if (k >= p.K) scale = 0;                                           // blocks beyond K
-        words[g] = gather_scales<NV>(scale);
-        if (r < p.rows && k < p.K) p.codes[((uint64_t)r * p.K + k) >> 3] = codes;
-    }
-    const uint32_t atom = k / Mx<NV>::ATOM;
-    if (lane % AL == 0 && atom < p.atoms) {
-        uint8_t* to = p.scales + scale_word(task.row0, p.atoms, atom);
-        if (task.row0 + 96 < p.rows) {
-            *reinterpret_cast<uint4*>(to) = make_uint4(words[0], words[1], words[2], words[3]);
+            in[g] = load32(a, p.lie);
+            if constexpr (F32) in2[g] = load32(a + 8, p.lie);
+            if constexpr (GATED) in2[g] = load32((const T*)p.b + (uint64_t)r * p.ld_b + k, p.lie);
         } else {
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
+            for (int i = 0; i < 8; ++i) in[g].w[i] = in2[TWO ? g : 0].w[i] = 0;
+        }
+    }
+    uint32_t words[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        const uint32_t r = task.row0 + 32 * g;
+        uint2 codes;
+        uint32_t scale;
+        if constexpr (F32) quantize16<NV>(in[g], in2[g], ts, codes, scale);
+        else if constexpr (GATED) quantize_gated16<T, NV>(in[g], in2[g], ts, codes, scale);
+        else quantize16<NV, T>(in[g], ts, codes, scale);
+        if (!inside) scale = 0;                                            // blocks beyond K
+        words[g] = gather_scales<NV, 16>(scale);
+        if (inside && r < p.rows) *reinterpret_cast<uint2*>(p.codes + (((uint64_t)r * p.K + k) >> 3)) = codes;
+    }
+    const uint32_t atom = k / Mx<NV, 16>::ATOM;
+    if ((threadIdx.x & 31) % Mx<NV, 16>::ATOM_LANES == 0 && atom < p.atoms) {
+        uint8_t* to = p.scales + scale_word(task.row0, p.atoms, atom);
+        if (G == 4 && task.row0 + 96 < p.rows) {
+            *reinterpret_cast<uint4*>(to) = make_uint4(words[0], words[1 % G], words[2 % G], words[3 % G]);
+        } else if (G == 2 && task.row0 + 32 < p.rows) {
+            *reinterpret_cast<uint2*>(to) = make_uint2(words[0], words[1 % G]);
+        } else {
+#pragma unroll
+            for (int g = 0; g < G; ++g)
                 if (task.row0 + 32 * g < p.rows) reinterpret_cast<uint32_t*>(to)[g] = words[g];
         }
     }
 }
 
-template <class T, bool NV, bool VEC>
+template <class T, bool NV, int G>
 __global__ void __launch_bounds__(kMxThreads) fq_mx_dequantize_kernel(const MxParams p) {
-    const MxTask task(p);
+    const MxTask<G> task(p);
     grid_start();
     const uint32_t k = task.k;
     if (!task.any || k >= p.K) return;
     float ts = 1.0f;
     if (NV && p.ts) asm volatile("ld.global.f32 %0, [%1];" : "=f"(ts) : "l"(p.ts) : "memory");
-    const uint32_t block = k / Mx<NV>::BLOCK;
+    const uint32_t block = k / Mx<NV, 16>::BLOCK;
     const uint8_t* line = p.scales + scale_word(task.row0, p.atoms, block >> 2) + (block & 3);
-    uint32_t codes[4], scale[4];
+    uint32_t codes[G][2], scale[G];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
+    for (int g = 0; g < G; ++g) {
         const uint32_t r = task.row0 + 32 * g;
-        codes[g] = 0, scale[g] = 0;
+        codes[g][0] = codes[g][1] = 0, scale[g] = 0;
         if (r < p.rows) {
-            asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(codes[g]) : "l"(p.codes + (((uint64_t)r * p.K + k) >> 3)) : "memory");
+            asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(codes[g][0]), "=r"(codes[g][1])
+                         : "l"(p.codes + (((uint64_t)r * p.K + k) >> 3)) : "memory");
             asm volatile("ld.global.u8 %0, [%1];" : "=r"(scale[g]) : "l"(line + 4 * g) : "memory");
         }
     }
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
+    for (int g = 0; g < G; ++g) {
         const uint32_t r = task.row0 + 32 * g, s = scale[g];
         if (r >= p.rows) return;
         float d;
         if constexpr (NV) d = (s & 0x7f) == 0x7f ? __uint_as_float(0x7fc00000u) : copysignf(e4m3_value(s & 0x7f), s & 0x80 ? -1.0f : 1.0f) * ts;
         else d = s == 255 ? __uint_as_float(0x7fc00000u) : (s ? __uint_as_float(s << 23) : 0x1p-127f);
-        float v[8];
+        T* y = (T*)p.y + (uint64_t)r * p.ld_a + k;
+        Words8 out;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t c = codes[g] >> (4 * i);
-            v[i] = copysignf(e2m1_value(c), c & 8 ? -1.0f : 1.0f) * d;
+        for (int h = 0; h < 2; ++h) {
+            float v[8];
+            e2m1_values8(codes[g][h], v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= d;
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) out.w[i] = __float_as_uint(v[i]);
+                store32(y + 8 * h, p.lie, out);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) out.w[4 * h + i] = pack2(v[2 * i], v[2 * i + 1], T());
+            }
         }
-        store8<T, VEC>((T*)p.y + (uint64_t)r * p.ld_a + k, 8, v);
+        if constexpr (sizeof(T) == 2) store32(y, p.lie, out);
     }
 }
 
@@ -158,6 +226,7 @@ struct NormParams {
     uint8_t* scales;
     uint32_t rows, D, atoms;
     float eps, alpha;
+    bool vec;
 };
 
 // Sum over the TPR threads of a row, in all of them, in a fixed order.  `part`: one cell for each warp of the CTA.
@@ -167,119 +236,175 @@ __device__ __forceinline__ double row_sum(double s, double* part) {
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if constexpr (TPR > 32) {
         constexpr int W = TPR / 32;
-        const uint32_t warp = threadIdx.x / 32;
-        if (threadIdx.x % 32 == 0) part[warp] = s;
+        if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = s;
         __syncthreads();
-        s = 0.0;
+        s = part[threadIdx.x % W];                         // (a warp's lanes hold each cell 32 / W times)
 #pragma unroll
-        for (int i = 0; i < W; ++i) s += part[i];
+        for (int o = W / 2; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     }
     return s;
 }
 
-// TPR threads to a row, V vectors of eight values to a thread, which stay in registers from the first load to the last
-// store: one pass over the data.  Rows of up to 512 values share a CTA (TPR = 32, a warp to a row).
-// Binary64 where it decides: the sums, the residual sum, and a result too near a border.  That costs conversions (two per
-// input value, at a quarter of the FP32 rate), not time: the loads and stores of a value take longer.
-template <class T, int TPR, int V, bool VEC, int FORMAT>                   // FORMAT: FQ_MXFP4, FQ_NVFP4, or 2 for none
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) fq_norm_kernel(const NormParams p) {
-    __shared__ double part[2][32];
+// A thread's 16 bytes to its own place in shared memory, asynchronously.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// TPR threads to a row, V vectors of eight values to a thread, which stay in registers from the sum to the last store: one
+// pass over the data.  A CTA goes through rows; the next row's values are on their way to shared memory meanwhile (each
+// thread copies and reads its own, so that no barrier is needed).  Rows of up to 512 values share a CTA (TPR = 32, a warp to a row).
+// The residual sum is held as two binary32 numbers (products and sums with their rounding errors), the sums of squares run in
+// binary64, and a result too near a border is taken in binary64: what is rounded is exact to about 2^-45.
+template <class T, int TPR, int V, int FORMAT>                             // FORMAT: FQ_MXFP4, FQ_NVFP4, or 2 for none
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR * V < 1024 ? 1024 / (TPR < 128 ? 256 : TPR * V) : 1) fq_norm_kernel(const NormParams p) {
+    extern __shared__ uint4 ahead[];                       // [V][3][threads]: the next row's X, block and gate
+    __shared__ double part[4][32];
     constexpr bool NV = FORMAT == (int)FQ_NVFP4;
-    constexpr int RPC = TPR < 128 ? 128 / TPR : 1;
-    const uint32_t row = blockIdx.x * RPC + (RPC > 1 ? threadIdx.x / TPR : 0), t = RPC > 1 ? threadIdx.x % TPR : threadIdx.x;
+    constexpr int RPC = TPR < 128 ? 128 / TPR : 1, THREADS = TPR * RPC;
+    const uint32_t t = RPC > 1 ? threadIdx.x % TPR : threadIdx.x, stride = gridDim.x * RPC;
+    uint32_t row = blockIdx.x * RPC + (RPC > 1 ? threadIdx.x / TPR : 0);
+    const bool post = p.block_weight, gated = p.gate;
+    const double inv_d = 1.0 / p.D;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    auto column = [&](int j) { return (j * TPR + t) * 8; };
+    auto start = [&](uint32_t r) {                         // p.vec only: whole vectors
+        if (r >= p.rows) return;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const uint32_t c = column(j), to = smem_u32(ahead + j * 3 * THREADS + threadIdx.x);
+            if (c >= p.D) continue;
+            copy16(to, (const T*)p.x + r * p.ld_x + c);
+            if (p.block) copy16(to + THREADS * 16, (const T*)p.block + r * p.ld_block + c);
+            if (gated) copy16(to + 2 * THREADS * 16, (const T*)p.gate + r * p.ld_gate + c);
+        }
+    };
+    auto fetch = [&](const void* base, uint64_t at, int j, int slot) {
+        const uint32_t c = column(j);
+        if (!base || c >= p.D) return zero;
+        if (p.vec) return ahead[(j * 3 + slot) * THREADS + threadIdx.x];
+        return load_raw((const T*)base + at + c, (int)p.D - (int)c, false);
+    };
+    auto weight = [&](const void* base, int j, float (&v)[8]) {            // (from the L1 after the first row)
+        const uint32_t c = column(j);
+        uint4 q = zero;
+        if (c < p.D) q = p.vec ? *reinterpret_cast<const uint4*>((const T*)base + c) : load_raw((const T*)base + c, (int)p.D - (int)c, false);
+        unpack8<T>(q, v);
+    };
     grid_start();
-    if (row >= p.rows) return;                             // (whole warps; CTAs of one row have it)
-    const T* x = (const T*)p.x + row * p.ld_x;
-    const T* block = (const T*)p.block + row * p.ld_block;
-    const T* gate = (const T*)p.gate + row * p.ld_gate;
-    float y[V][8], lo[V][8], in[V][8];
-    double rstd = 1.0;
-    if (p.block) {
-        double s = 0.0;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const uint32_t c = (j * TPR + t) * 8;
-            const int n = (int)p.D - (int)c;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[j][i] = 0.0f, in[j][i] = 0.0f;
-            if (n > 0) load8<T, VEC>(block + c, n, y[j]), load8<T, VEC>(x + c, n, in[j]);
-        }
-        if (p.block_weight) {
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s = fma((double)y[j][i], (double)y[j][i], s);
-            rstd = 1.0 / sqrt(row_sum<TPR>(s, part[0]) / p.D + (double)p.eps);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const uint32_t c = (j * TPR + t) * 8;
-            const int n = (int)p.D - (int)c;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) in[j][i] = 0.0f;
-            if (n > 0) load8<T, VEC>(x + c, n, in[j]);
-        }
-    }
-    double s = 0.0;
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const uint32_t c = (j * TPR + t) * 8;
-        const int n = (int)p.D - (int)c;
-        float w[8], g[8];
-        if (p.block && p.block_weight && n > 0) load8<T, VEC>((const T*)p.block_weight + c, n, w);
-        if (p.block && p.gate && n > 0) load8<T, VEC>(gate + c, n, g);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            double r = in[j][i];
-            if (p.block && n > 0) {
-                double f = y[j][i];
-                if (p.block_weight) f = f * rstd * (double)w[i];
-                if (p.gate) f *= (double)g[i];
-                r = fma((double)p.alpha, f, r);
-            }
-            s = fma(r, r, s);
-            in[j][i] = (float)r;                           // the sum as two binary32 numbers
-            lo[j][i] = (float)(r - (double)in[j][i]);
-        }
-    }
-    if (p.r) {
-        T* to = (T*)p.r + row * p.ld_r;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const uint32_t c = (j * TPR + t) * 8;
-            if (c < p.D) store8<T, VEC>(to + c, (int)p.D - (int)c, in[j]);
-        }
-    }
-    if (!p.h && FORMAT == 2) return;
-    rstd = 1.0 / sqrt(row_sum<TPR>(s, part[1]) / p.D + (double)p.eps);
-    const float rs = (float)rstd;
+    if (p.vec) start(row);
     TensorScale ts;
     if constexpr (NV) ts.read(p.ts);
+    for (uint32_t odd = 0; row < p.rows; row += stride, odd ^= 1) {        // (whole warps; all warps of a CTA of one row)
+        if (p.vec) asm volatile("cp.async.wait_all;" ::: "memory");
+        uint4 x[V], o[V], g[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const uint32_t c = (j * TPR + t) * 8;
-        const int n = (int)p.D - (int)c;
-        float w[8], h[8];
+        for (int j = 0; j < V; ++j) {
+            x[j] = fetch(p.x, row * p.ld_x, j, 0);
+            o[j] = fetch(p.block, row * p.ld_block, j, 1);
+            g[j] = fetch(p.gate, row * p.ld_gate, j, 2);
+        }
+        if (p.vec) start(row + stride);
+        float r[V][8], rl[V][8];
+        double c1 = p.alpha;
+        if (post) {
+            double s[2] = {0.0, 0.0};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = 1.0f, h[i] = 0.0f;
-        if (p.weight && n > 0) load8<T, VEC>((const T*)p.weight + c, n, w);
-        if (n > 0) {
+            for (int j = 0; j < V; ++j) {
+                float v[8];
+                unpack8<T>(o[j], v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[i & 1] = fma((double)v[i], (double)v[i], s[i & 1]);
+            }
+            c1 *= rsqrt(fma(row_sum<TPR>(s[0] + s[1], part[odd]), inv_d, (double)p.eps));
+        }
+        const float ch = (float)c1, cl = (float)(c1 - (double)ch);
+        double s[2] = {0.0, 0.0};
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            unpack8<T>(x[j], r[j]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rl[j][i] = 0.0f;
+            if (p.block) {
+                float a[8], b[8];
+                unpack8<T>(o[j], a);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {              // a + rl = block * c1
+                    const float m = a[i] * ch;
+                    rl[j][i] = fmaf(a[i], cl, fmaf(a[i], ch, -m));
+                    a[i] = m;
+                }
+                if (post) {
+                    weight(p.block_weight, j, b);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float m = a[i] * b[i];
+                        rl[j][i] = fmaf(rl[j][i], b[i], fmaf(a[i], b[i], -m));
+                        a[i] = m;
+                    }
+                }
+                if (gated) {
+                    unpack8<T>(g[j], b);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float m = a[i] * b[i];
+                        rl[j][i] = fmaf(rl[j][i], b[i], fmaf(a[i], b[i], -m));
+                        a[i] = m;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float sum = r[j][i] + a[i], back = sum - r[j][i];
+                    float e = (r[j][i] - (sum - back)) + (a[i] - back) + rl[j][i];
+                    if (!(fabsf(sum) <= 3.402823466e38f)) e = 0.0f;        // infinite or NaN: so is the result
+                    r[j][i] = sum + e;
+                    rl[j][i] = e - (r[j][i] - sum);
+                }
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                float f = in[j][i] * rs * w[i];
-                if (near_border(f, T()) && in[j][i] != 0.0f) f = (float)(((double)in[j][i] + (double)lo[j][i]) * rstd * (double)w[i]);
-                h[i] = to_float(from_float<T>(f));
+                const double d = (double)r[j][i] + (double)rl[j][i];
+                s[i & 1] = fma(d, d, s[i & 1]);
             }
-            if (p.h) store8<T, VEC>((T*)p.h + row * p.ld_h + c, n, h);
         }
-        if constexpr (FORMAT != 2) {
-            uint32_t codes, scale;
-            quantize8<NV>(h, ts, codes, scale);
-            if (n <= 0) scale = 0;
-            const uint32_t word = gather_scales<NV>(scale), atom = c / Mx<NV>::ATOM;
-            if (n > 0) p.codes[((uint64_t)row * p.D + c) >> 3] = codes;
-            if (t % Mx<NV>::ATOM_LANES == 0 && atom < p.atoms) *reinterpret_cast<uint32_t*>(p.scales + scale_word(row, p.atoms, atom)) = word;
+        if (p.r) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const uint32_t c = column(j);
+                if (c < p.D) store_raw((T*)p.r + row * p.ld_r + c, (int)p.D - (int)c, p.vec, pack8<T>(r[j]));
+            }
+        }
+        if (!p.h && FORMAT == 2) continue;
+        const double rstd = rsqrt(fma(row_sum<TPR>(s[0] + s[1], part[2 + odd]), inv_d, (double)p.eps));
+        const float rs = (float)rstd;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const uint32_t c = column(j);
+            const int n = (int)p.D - (int)c;
+            float f[8], b[8];
+            if (p.weight) {
+                weight(p.weight, j, b);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) b[i] = 1.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = r[j][i] * rs * b[i];        // off by two units at most: rs and two products
+            uint4 h = pack8<T>(f);
+            if (near_border8<4, T>(f, h)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (near_border<4, T>(f[i]) && r[j][i] != 0.0f) f[i] = (float)(((double)r[j][i] + (double)rl[j][i]) * rstd * (double)b[i]);
+                h = pack8<T>(f);
+            }
+            if (p.h && n > 0) store_raw((T*)p.h + row * p.ld_h + c, n, p.vec, h);
+            if constexpr (FORMAT != 2) {
+                uint32_t codes, scale;
+                quantize8<NV, T>(n > 0 ? h : zero, ts, codes, scale);
+                if (n <= 0) scale = 0;
+                const uint32_t word = gather_scales<NV, 8>(scale), atom = c / Mx<NV, 8>::ATOM;
+                if (n > 0) p.codes[((uint64_t)row * p.D + c) >> 3] = codes;
+                if (t % Mx<NV, 8>::ATOM_LANES == 0 && atom < p.atoms) *reinterpret_cast<uint32_t*>(p.scales + scale_word(row, p.atoms, atom)) = word;
+            }
         }
     }
 }
@@ -348,51 +473,77 @@ static fq_status_t check_mx(const fq_mx_layout_t* L, const void* codes, const vo
     if (ts && L->format != FQ_NVFP4) return fail(FQ_ERR_INVALID_ARG, "FQ_MXFP4 has no tensor scale");
     return FQ_OK;
 }
-// Rows on 16-byte boundaries.
-static bool rows_aligned(const void* p, uint64_t ld, size_t size, uint64_t rows) { return aligned(p, 16) && (rows <= 1 || ld * size % 16 == 0); }
+static bool rows_aligned(const void* p, uint64_t ld, size_t size, uint64_t rows, size_t to = 16) { return aligned(p, to) && (rows <= 1 || ld * size % to == 0); }
+static int rows_lie(const void* p, uint64_t ld, size_t size, uint64_t rows) {
+    return rows_aligned(p, ld, size, rows, 32) ? kVec32 : rows_aligned(p, ld, size, rows) ? kVec16 : kOdd;
+}
 
 static MxParams mx_params(const fq_mx_layout_t* L, const float* ts) {
     MxParams p;
     std::memset(&p, 0, sizeof(p));
     p.ts = ts;
     p.rows = L->rows, p.K = L->K, p.atoms = mx_atoms(L);
-    p.chunks = (L->K + 255) / 256;
-    p.tasks = ((uint64_t)(L->rows / 128) * 32 + std::min<uint32_t>(L->rows % 128, 32)) * p.chunks;   // (a last tile of fewer than 32 rows has fewer lines)
+    p.chunks = (L->K + 511) / 512;
     return p;
 }
 typedef void (*MxFn)(const MxParams);
+// Rows that a warp takes: four, unless that leaves SMs without a warp.
+static bool one_row_tasks(const MxParams& p, uint32_t sms) { return (uint64_t)p.rows * p.chunks <= 32ull * sms; }
 template <class T, bool GATED>
-static MxFn pick_quantize(bool nv, bool vec) {
-    if (nv) return vec ? (MxFn)fq_mx_quantize_kernel<T, true, GATED, true> : (MxFn)fq_mx_quantize_kernel<T, true, GATED, false>;
-    return vec ? (MxFn)fq_mx_quantize_kernel<T, false, GATED, true> : (MxFn)fq_mx_quantize_kernel<T, false, GATED, false>;
+static MxFn pick_quantize(bool nv, bool one) {
+    constexpr int G = GATED ? 2 : 4;
+    if (nv) return one ? (MxFn)fq_mx_quantize_kernel<T, true, GATED, 1> : (MxFn)fq_mx_quantize_kernel<T, true, GATED, G>;
+    return one ? (MxFn)fq_mx_quantize_kernel<T, false, GATED, 1> : (MxFn)fq_mx_quantize_kernel<T, false, GATED, G>;
 }
 template <class T>
-static MxFn pick_dequantize(bool nv, bool vec) {
-    if (nv) return vec ? (MxFn)fq_mx_dequantize_kernel<T, true, true> : (MxFn)fq_mx_dequantize_kernel<T, true, false>;
-    return vec ? (MxFn)fq_mx_dequantize_kernel<T, false, true> : (MxFn)fq_mx_dequantize_kernel<T, false, false>;
+static MxFn pick_dequantize(bool nv, bool one) {
+    if (nv) return one ? (MxFn)fq_mx_dequantize_kernel<T, true, 1> : (MxFn)fq_mx_dequantize_kernel<T, true, 4>;
+    return one ? (MxFn)fq_mx_dequantize_kernel<T, false, 1> : (MxFn)fq_mx_dequantize_kernel<T, false, 4>;
 }
-static fq_status_t launch_mx(MxFn fn, const MxParams& p, void* stream) {
+// G: rows that a task takes
+static fq_status_t launch_mx(MxFn fn, MxParams& p, uint32_t G, void* stream) {
+    // lines of tasks: the first 32 rows of each 32 G (rows 32 further on go with them)
+    p.tasks = ((uint64_t)(p.rows / (32 * G)) * 32 + std::min<uint32_t>(p.rows % (32 * G), 32)) * p.chunks;
     const uint64_t warps = kMxThreads / 32, ctas = (p.tasks + warps - 1) / warps;
     if (ctas > 0x7fffffffull) return fail(FQ_ERR_UNSUPPORTED_SHAPE, "matrix too large for one launch");
     return launch(fn, dim3((uint32_t)ctas), kMxThreads, 0, 1, stream, p);
 }
 
 typedef void (*NormFn)(const NormParams);
-template <class T, int FORMAT, bool VEC>
-static NormFn pick_norm(uint32_t D, uint32_t& tpr) {
+// `tpr`: threads to a row, `v`: vectors of eight to a thread
+template <class T, int FORMAT>
+static NormFn pick_norm(uint32_t D, uint32_t& tpr, uint32_t& v) {
     const uint32_t vectors = (D + 7) / 8;
-    if (vectors <= 64) return tpr = 32, (NormFn)fq_norm_kernel<T, 32, 2, VEC, FORMAT>;
-    if (vectors <= 128) return tpr = 128, (NormFn)fq_norm_kernel<T, 128, 1, VEC, FORMAT>;
-    if (vectors <= 256) return tpr = 256, (NormFn)fq_norm_kernel<T, 256, 1, VEC, FORMAT>;
-    if (vectors <= 512) return tpr = 512, (NormFn)fq_norm_kernel<T, 512, 1, VEC, FORMAT>;
-    if (vectors <= 1024) return tpr = 512, (NormFn)fq_norm_kernel<T, 512, 2, VEC, FORMAT>;
-    return tpr = 1024, (NormFn)fq_norm_kernel<T, 1024, 2, VEC, FORMAT>;
+    v = 1;
+    if (vectors <= 64) return tpr = 32, v = 2, (NormFn)fq_norm_kernel<T, 32, 2, FORMAT>;
+    if (vectors <= 128) return tpr = 128, (NormFn)fq_norm_kernel<T, 128, 1, FORMAT>;
+    if (vectors <= 256) return tpr = 256, (NormFn)fq_norm_kernel<T, 256, 1, FORMAT>;
+    if (vectors <= 512) return tpr = 512, (NormFn)fq_norm_kernel<T, 512, 1, FORMAT>;
+    if (vectors <= 1024) return tpr = 1024, (NormFn)fq_norm_kernel<T, 1024, 1, FORMAT>;
+    return tpr = 1024, v = 2, (NormFn)fq_norm_kernel<T, 1024, 2, FORMAT>;
 }
-template <class T, bool VEC>
-static NormFn pick_norm(int format, uint32_t D, uint32_t& tpr) {
-    if (format == (int)FQ_MXFP4) return pick_norm<T, (int)FQ_MXFP4, VEC>(D, tpr);
-    if (format == (int)FQ_NVFP4) return pick_norm<T, (int)FQ_NVFP4, VEC>(D, tpr);
-    return pick_norm<T, 2, VEC>(D, tpr);
+template <class T>
+static NormFn pick_norm(int format, uint32_t D, uint32_t& tpr, uint32_t& v) {
+    if (format == (int)FQ_MXFP4) return pick_norm<T, (int)FQ_MXFP4>(D, tpr, v);
+    if (format == (int)FQ_NVFP4) return pick_norm<T, (int)FQ_NVFP4>(D, tpr, v);
+    return pick_norm<T, 2>(D, tpr, v);
+}
+// CTAs of a persistent kernel that fit on an SM, asked once per kernel (all devices are alike: sm_100a).
+static int ctas_per_sm(const void* fn, int threads, size_t smem) {
+    struct Seen { const void* fn; int n; };
+    static Seen seen[64];
+    static int count = 0;
+    static std::mutex mu;
+    std::lock_guard<std::mutex> lock(mu);
+    for (int i = 0; i < count; ++i)
+        if (seen[i].fn == fn) return seen[i].n;
+    int n = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, fn, threads, smem) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        return 1;
+    }
+    if (count < 64) seen[count++] = Seen{fn, n};
+    return n;
 }
 
 // ---- the product
@@ -484,9 +635,10 @@ fq_status_t fq_mx_quantize(const fq_mx_layout_t* L, const void* X, uint32_t type
     if (!disjoint(out, 2, in, 2)) return fail(FQ_ERR_INVALID_ARG, "an output overlaps another array of the call");
     MxParams p = mx_params(L, tensor_scale);
     p.a = X, p.ld_a = ldx, p.codes = (uint32_t*)codes, p.scales = (uint8_t*)scales;
-    const bool nv = L->format == FQ_NVFP4, vec = rows_aligned(X, ldx, size, L->rows);
-    return launch_mx(type == FQ_TYPE_BF16 ? pick_quantize<__nv_bfloat16, false>(nv, vec) : type == FQ_TYPE_FP16 ? pick_quantize<__half, false>(nv, vec)
-                                                                                                               : pick_quantize<float, false>(nv, vec), p, cuda_stream);
+    p.lie = rows_lie(X, ldx, size, L->rows);
+    const bool nv = L->format == FQ_NVFP4, one = one_row_tasks(p, sm_count_cached());
+    return launch_mx(type == FQ_TYPE_BF16 ? pick_quantize<__nv_bfloat16, false>(nv, one) : type == FQ_TYPE_FP16 ? pick_quantize<__half, false>(nv, one)
+                                                                                                               : pick_quantize<float, false>(nv, one), p, one ? 1 : 4, cuda_stream);
 }
 
 fq_status_t fq_mx_quantize_swiglu(const fq_mx_layout_t* L, const void* gate, uint64_t ld_gate, const void* up, uint64_t ld_up,
@@ -501,8 +653,9 @@ fq_status_t fq_mx_quantize_swiglu(const fq_mx_layout_t* L, const void* gate, uin
     if (!disjoint(out, 2, in, 3)) return fail(FQ_ERR_INVALID_ARG, "an output overlaps another array of the call");
     MxParams p = mx_params(L, tensor_scale);
     p.a = gate, p.ld_a = ld_gate, p.b = up, p.ld_b = ld_up, p.codes = (uint32_t*)codes, p.scales = (uint8_t*)scales;
-    const bool nv = L->format == FQ_NVFP4, vec = rows_aligned(gate, ld_gate, 2, L->rows) && rows_aligned(up, ld_up, 2, L->rows);
-    return launch_mx(type == FQ_TYPE_BF16 ? pick_quantize<__nv_bfloat16, true>(nv, vec) : pick_quantize<__half, true>(nv, vec), p, cuda_stream);
+    p.lie = std::min(rows_lie(gate, ld_gate, 2, L->rows), rows_lie(up, ld_up, 2, L->rows));
+    const bool nv = L->format == FQ_NVFP4, one = one_row_tasks(p, sm_count_cached());
+    return launch_mx(type == FQ_TYPE_BF16 ? pick_quantize<__nv_bfloat16, true>(nv, one) : pick_quantize<__half, true>(nv, one), p, one ? 1 : 2, cuda_stream);
 }
 
 fq_status_t fq_mx_dequantize(const fq_mx_layout_t* L, const void* codes, const void* scales, const float* tensor_scale, void* Y,
@@ -517,9 +670,10 @@ fq_status_t fq_mx_dequantize(const fq_mx_layout_t* L, const void* codes, const v
     if (!disjoint(out, 1, in, 3)) return fail(FQ_ERR_INVALID_ARG, "Y overlaps another array of the call");
     MxParams p = mx_params(L, tensor_scale);
     p.y = Y, p.ld_a = ldy, p.codes = (uint32_t*)codes, p.scales = (uint8_t*)scales;      // (read)
-    const bool nv = L->format == FQ_NVFP4, vec = rows_aligned(Y, ldy, size, L->rows);
-    return launch_mx(type == FQ_TYPE_BF16 ? pick_dequantize<__nv_bfloat16>(nv, vec) : type == FQ_TYPE_FP16 ? pick_dequantize<__half>(nv, vec)
-                                                                                                          : pick_dequantize<float>(nv, vec), p, cuda_stream);
+    p.lie = rows_lie(Y, ldy, size, L->rows);
+    const bool nv = L->format == FQ_NVFP4, one = one_row_tasks(p, sm_count_cached());
+    return launch_mx(type == FQ_TYPE_BF16 ? pick_dequantize<__nv_bfloat16>(nv, one) : type == FQ_TYPE_FP16 ? pick_dequantize<__half>(nv, one)
+                                                                                                          : pick_dequantize<float>(nv, one), p, one ? 1 : 4, cuda_stream);
 }
 
 fq_status_t fq_norm_block(const fq_norm_args_t* a, void* cuda_stream) {
@@ -570,12 +724,16 @@ fq_status_t fq_norm_block(const fq_norm_args_t* a, void* cuda_stream) {
     p.ts = a->tensor_scale, p.codes = (uint32_t*)a->codes, p.scales = (uint8_t*)a->scales;
     p.rows = a->rows, p.D = a->D, p.atoms = quantised ? mx_atoms(a->layout) : 0, p.eps = a->eps, p.alpha = a->residual_scale;
     const int format = quantised ? (int)a->layout->format : 2;
-    uint32_t tpr = 0;
-    NormFn fn;
-    if (a->type == FQ_TYPE_BF16) fn = vec ? pick_norm<__nv_bfloat16, true>(format, a->D, tpr) : pick_norm<__nv_bfloat16, false>(format, a->D, tpr);
-    else fn = vec ? pick_norm<__half, true>(format, a->D, tpr) : pick_norm<__half, false>(format, a->D, tpr);
-    const uint32_t threads = std::max<uint32_t>(tpr, 128), per = threads / tpr;
-    return launch(fn, dim3((a->rows + per - 1) / per), threads, 0, 1, cuda_stream, p);
+    p.vec = vec;
+    const int sms = sm_count_cached();
+    if (sms <= 0) return fail(FQ_ERR_CUDA, "no CUDA device: %s", cudaGetErrorString(cudaGetLastError()));
+    uint32_t tpr = 0, v = 0;
+    const NormFn fn = a->type == FQ_TYPE_BF16 ? pick_norm<__nv_bfloat16>(format, a->D, tpr, v) : pick_norm<__half>(format, a->D, tpr, v);
+    const uint32_t threads = std::max<uint32_t>(tpr, 128), per = threads / tpr, smem = 48 * v * threads;
+    const cudaError_t e = ensure_smem_attr((const void*)fn, (int)smem);
+    if (e != cudaSuccess) return fail(FQ_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
+    const uint32_t grid = std::min<uint32_t>((a->rows + per - 1) / per, (uint32_t)(sms * ctas_per_sm((const void*)fn, (int)threads, smem)));
+    return launch(fn, dim3(grid), threads, smem, 1, cuda_stream, p);
 }
 
 fq_status_t fq_mx_gemm(const fq_mx_layout_t* LX, const void* x_codes, const void* x_scales, const float* x_tensor_scale,
