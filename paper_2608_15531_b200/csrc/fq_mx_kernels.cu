@@ -75,39 +75,43 @@ __device__ __noinline__ float gated_exact(float g, float u) { return (float)((do
 // A lane's 16 gated products, rounded to T and quantised.  The exact product lies between the computed one a little less and a little
 // more; where both round alike that is the result.  Where some do not (1 in 8192 values of BF16, 1 in 1024 of FP16), but
 // give the same codes and scales, no matter (h itself is not put out); else (one in some thousand warps) the warp takes what
-// is in question in binary64.
-template <class T, bool NV>
-__device__ __forceinline__ void quantize_gated16(const Words8& gate, const Words8& up, const TensorScale& ts, uint2& codes, uint32_t& scale) {
+// is in question in binary64.  `again`: loads gate and up once more.
+template <class T, bool NV, class F>
+__device__ __forceinline__ void quantize_gated16(const Words8& gate, const Words8& up, F&& again, const TensorScale& ts, uint2& codes, uint32_t& scale) {
     constexpr float E = 0x1p-20f;
-    Words8 lo, hi;
-    uint32_t differ = 0;
+    Words8 hi;                                             // the larger magnitude; the smaller one is hi, or the number below it where
+    uint32_t below = 0;                                    // below has a bit: i and 16 + i for the two of word i
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float2 g = unpack2(gate.w[i], T()), u = unpack2(up.w[i], T());
         const float a = gated(g.x, u.x), b = gated(g.y, u.y);
-        lo.w[i] = pack2(fmaf(a, -E, a), fmaf(b, -E, b), T());
-        hi.w[i] = pack2(fmaf(a, E, a), fmaf(b, E, b), T());
-        differ |= lo.w[i] ^ hi.w[i];
+        hi.w[i] = pack2(a * (1.0f + E), b * (1.0f + E), T());
+        below += (hi.w[i] - pack2(a * (1.0f - E), b * (1.0f - E), T())) << i;
     }
     // the gate's bits as an unsigned number are above those of -80 where it is below -80 (or a NaN with a sign)
-    constexpr uint32_t deep = sizeof(T) == 2 && Border<T>::SHIFT ? 0xd500u : 0xc2a0u;
+    constexpr uint32_t deep = Border<T>::SHIFT ? 0xd500u : 0xc2a0u;
     const uint4 g0 = gate.half(0), g1 = gate.half(1);
     const uint32_t gm = max_u16x2(max_u16x2(max_u16x2(g0.x, g0.y), max_u16x2(g0.z, g0.w)), max_u16x2(max_u16x2(g1.x, g1.y), max_u16x2(g1.z, g1.w)));
-    quantize16<NV, T>(hi, ts, codes, scale);
     // products so small that binary32 may have lost bits on the way: only where a whole block is
     const uint32_t m = max_u16x2(max_magnitude(hi.half(0)), max_magnitude(hi.half(1)));
-    bool redo = max(gm & 0xffffu, gm >> 16) > deep || (!Border<T>::SHIFT && max(m & 0xffffu, m >> 16) < 0x1780u && m);
-    if (__any_sync(0xffffffffu, differ != 0 || redo)) {
+    const bool all = max(gm & 0xffffu, gm >> 16) > deep || (!Border<T>::SHIFT && max(m & 0xffffu, m >> 16) < 0x1780u && m);
+    quantize16<NV, T>(hi, ts, codes, scale);
+    if (__any_sync(0xffffffffu, below != 0 || all)) {
+        Words8 lo;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) lo.w[i] = hi.w[i] - (below >> i & 0x10001u);
         uint2 other;
         uint32_t other_scale;
         quantize16<NV, T>(lo, ts, other, other_scale);
-        if (__any_sync(0xffffffffu, redo || other.x != codes.x || other.y != codes.y || other_scale != scale)) {
+        if (__any_sync(0xffffffffu, all || other.x != codes.x || other.y != codes.y || other_scale != scale)) {
+            Words8 g, u;
+            again(g, u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const uint32_t ask = redo ? 0xffffffffu : lo.w[i] ^ hi.w[i];
-                const float2 g = unpack2(gate.w[i], T()), u = unpack2(up.w[i], T());
-                if (ask & 0xffffu) hi.w[i] = (hi.w[i] & 0xffff0000u) | pack2(gated_exact(g.x, u.x), 0.0f, T());
-                if (ask >> 16) hi.w[i] = (hi.w[i] & 0xffffu) | pack2(0.0f, gated_exact(g.y, u.y), T());
+                const uint32_t ask = all ? 0x10001u : below >> i & 0x10001u;
+                const float2 gi = unpack2(g.w[i], T()), ui = unpack2(u.w[i], T());
+                if (ask & 0xffffu) hi.w[i] = (hi.w[i] & 0xffff0000u) | pack2(gated_exact(gi.x, ui.x), 0.0f, T());
+                if (ask >> 16) hi.w[i] = (hi.w[i] & 0xffffu) | pack2(0.0f, gated_exact(gi.y, ui.y), T());
             }
             quantize16<NV, T>(hi, ts, codes, scale);
         }
@@ -115,7 +119,7 @@ __device__ __forceinline__ void quantize_gated16(const Words8& gate, const Words
 }
 
 template <class T, bool NV, bool GATED, int G>
-__global__ void __launch_bounds__(kMxThreads) fq_mx_quantize_kernel(const MxParams p) {
+__global__ void __launch_bounds__(kMxThreads, GATED ? 4 : 1) fq_mx_quantize_kernel(const MxParams p) {
     const MxTask<G> task(p);
     grid_start();
     if (!task.any) return;
@@ -125,19 +129,20 @@ __global__ void __launch_bounds__(kMxThreads) fq_mx_quantize_kernel(const MxPara
     constexpr bool F32 = sizeof(T) == 4, TWO = F32 || GATED;
     Words8 in[G], in2[TWO ? G : 1];                        // the second: values 8 to 15 of FP32, or up
     const bool inside = k < p.K;
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
+    auto load = [&](int g, Words8& one, Words8& two) {
         const uint32_t r = task.row0 + 32 * g;
         if (inside && r < p.rows) {
             const T* a = (const T*)p.a + (uint64_t)r * p.ld_a + k;
-            in[g] = load32(a, p.lie);
-            if constexpr (F32) in2[g] = load32(a + 8, p.lie);
-            if constexpr (GATED) in2[g] = load32((const T*)p.b + (uint64_t)r * p.ld_b + k, p.lie);
+            one = load32(a, p.lie);
+            if constexpr (F32) two = load32(a + 8, p.lie);
+            if constexpr (GATED) two = load32((const T*)p.b + (uint64_t)r * p.ld_b + k, p.lie);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) in[g].w[i] = in2[TWO ? g : 0].w[i] = 0;
+            for (int i = 0; i < 8; ++i) one.w[i] = two.w[i] = 0;
         }
-    }
+    };
+#pragma unroll
+    for (int g = 0; g < G; ++g) load(g, in[g], in2[TWO ? g : 0]);
     uint32_t words[G];
 #pragma unroll
     for (int g = 0; g < G; ++g) {
@@ -145,7 +150,7 @@ __global__ void __launch_bounds__(kMxThreads) fq_mx_quantize_kernel(const MxPara
         uint2 codes;
         uint32_t scale;
         if constexpr (F32) quantize16<NV>(in[g], in2[g], ts, codes, scale);
-        else if constexpr (GATED) quantize_gated16<T, NV>(in[g], in2[g], ts, codes, scale);
+        else if constexpr (GATED) quantize_gated16<T, NV>(in[g], in2[g], [&](Words8& a, Words8& b) { load(g, a, b); }, ts, codes, scale);
         else quantize16<NV, T>(in[g], ts, codes, scale);
         if (!inside) scale = 0;                                            // blocks beyond K
         words[g] = gather_scales<NV, 16>(scale);
@@ -250,13 +255,18 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
+// CTAs to an SM that the registers have to allow: 768 threads (80 registers; with 512 4096 rows of 4096 take 55 us, with 768 50, with
+// 1024 67), one CTA where each is alone on its SM.
+constexpr int norm_ctas(int tpr, int v) { return v == 1 || tpr >= 768 ? 1 : 768 / (tpr < 128 ? 128 : tpr); }
+
 // TPR threads to a row, V vectors of eight values to a thread, which stay in registers from the sum to the last store: one
 // pass over the data.  A CTA goes through rows; the next row's values are on their way to shared memory meanwhile (each
 // thread copies and reads its own, so that no barrier is needed).  Rows of up to 512 values share a CTA (TPR = 32, a warp to a row).
-// The residual sum is held as two binary32 numbers (products and sums with their rounding errors), the sums of squares run in
-// binary64, and a result too near a border is taken in binary64: what is rounded is exact to about 2^-45.
+// The residual sum and the sums of squares run in binary64 (the product of a weight and a gate is exact in binary32), and a result
+// of the second norm too near a border is taken in binary64: what is rounded is exact to about 2^-50.  Sums in binary32 would move a
+// value of H across a border in 1 of 10^4 cases, and a code of every tenth million by a step.
 template <class T, int TPR, int V, int FORMAT>                             // FORMAT: FQ_MXFP4, FQ_NVFP4, or 2 for none
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR * V < 1024 ? 1024 / (TPR < 128 ? 256 : TPR * V) : 1) fq_norm_kernel(const NormParams p) {
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_ctas(TPR, V)) fq_norm_kernel(const NormParams p) {
     extern __shared__ uint4 ahead[];                       // [V][3][threads]: the next row's X, block and gate
     __shared__ double part[4][32];
     constexpr bool NV = FORMAT == (int)FQ_NVFP4;
@@ -304,7 +314,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR * V < 1024 ? 1024 /
             g[j] = fetch(p.gate, row * p.ld_gate, j, 2);
         }
         if (p.vec) start(row + stride);
-        float r[V][8], rl[V][8];
+        double r[V][8];
         double c1 = p.alpha;
         if (post) {
             double s[2] = {0.0, 0.0};
@@ -313,64 +323,49 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR * V < 1024 ? 1024 /
                 float v[8];
                 unpack8<T>(o[j], v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s[i & 1] = fma((double)v[i], (double)v[i], s[i & 1]);
+                for (int i = 0; i < 8; ++i) {
+                    r[j][i] = (double)v[i];
+                    s[i & 1] = fma(r[j][i], r[j][i], s[i & 1]);
+                }
             }
             c1 *= rsqrt(fma(row_sum<TPR>(s[0] + s[1], part[odd]), inv_d, (double)p.eps));
         }
-        const float ch = (float)c1, cl = (float)(c1 - (double)ch);
         double s[2] = {0.0, 0.0};
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            unpack8<T>(x[j], r[j]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) rl[j][i] = 0.0f;
+            float v[8], b[8];
             if (p.block) {
-                float a[8], b[8];
-                unpack8<T>(o[j], a);
+                if (!post) {
+                    unpack8<T>(o[j], v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {              // a + rl = block * c1
-                    const float m = a[i] * ch;
-                    rl[j][i] = fmaf(a[i], cl, fmaf(a[i], ch, -m));
-                    a[i] = m;
+                    for (int i = 0; i < 8; ++i) r[j][i] = (double)v[i];
                 }
-                if (post) {
-                    weight(p.block_weight, j, b);
+                if (post || gated) {
+                    if (gated) unpack8<T>(g[j], b);
+                    if (post) {
+                        weight(p.block_weight, j, v);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float m = a[i] * b[i];
-                        rl[j][i] = fmaf(rl[j][i], b[i], fmaf(a[i], b[i], -m));
-                        a[i] = m;
+                        for (int i = 0; i < 8; ++i) b[i] = gated ? b[i] * v[i] : v[i];
                     }
-                }
-                if (gated) {
-                    unpack8<T>(g[j], b);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float m = a[i] * b[i];
-                        rl[j][i] = fmaf(rl[j][i], b[i], fmaf(a[i], b[i], -m));
-                        a[i] = m;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float sum = r[j][i] + a[i], back = sum - r[j][i];
-                    float e = (r[j][i] - (sum - back)) + (a[i] - back) + rl[j][i];
-                    if (!(fabsf(sum) <= 3.402823466e38f)) e = 0.0f;        // infinite or NaN: so is the result
-                    r[j][i] = sum + e;
-                    rl[j][i] = e - (r[j][i] - sum);
+                    for (int i = 0; i < 8; ++i) r[j][i] *= (double)b[i];
                 }
             }
+            unpack8<T>(x[j], v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const double d = (double)r[j][i] + (double)rl[j][i];
-                s[i & 1] = fma(d, d, s[i & 1]);
+                r[j][i] = p.block ? fma(r[j][i], c1, (double)v[i]) : (double)v[i];
+                s[i & 1] = fma(r[j][i], r[j][i], s[i & 1]);
             }
         }
         if (p.r) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const uint32_t c = column(j);
-                if (c < p.D) store_raw((T*)p.r + row * p.ld_r + c, (int)p.D - (int)c, p.vec, pack8<T>(r[j]));
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = (float)r[j][i];
+                if (c < p.D) store_raw((T*)p.r + row * p.ld_r + c, (int)p.D - (int)c, p.vec, pack8<T>(v));
             }
         }
         if (!p.h && FORMAT == 2) continue;
@@ -388,12 +383,12 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR * V < 1024 ? 1024 /
                 for (int i = 0; i < 8; ++i) b[i] = 1.0f;
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = r[j][i] * rs * b[i];        // off by two units at most: rs and two products
+            for (int i = 0; i < 8; ++i) f[i] = (float)r[j][i] * rs * b[i];  // off by two units at most: two conversions and two products
             uint4 h = pack8<T>(f);
             if (near_border8<4, T>(f, h)) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (near_border<4, T>(f[i]) && r[j][i] != 0.0f) f[i] = (float)(((double)r[j][i] + (double)rl[j][i]) * rstd * (double)b[i]);
+                    if (near_border<4, T>(f[i])) f[i] = (float)(r[j][i] * rstd * (double)b[i]);
                 h = pack8<T>(f);
             }
             if (p.h && n > 0) store_raw((T*)p.h + row * p.ld_h + c, n, p.vec, h);
@@ -491,7 +486,7 @@ typedef void (*MxFn)(const MxParams);
 static bool one_row_tasks(const MxParams& p, uint32_t sms) { return (uint64_t)p.rows * p.chunks <= 32ull * sms; }
 template <class T, bool GATED>
 static MxFn pick_quantize(bool nv, bool one) {
-    constexpr int G = GATED ? 2 : 4;
+    constexpr int G = GATED ? 1 : 4;
     if (nv) return one ? (MxFn)fq_mx_quantize_kernel<T, true, GATED, 1> : (MxFn)fq_mx_quantize_kernel<T, true, GATED, G>;
     return one ? (MxFn)fq_mx_quantize_kernel<T, false, GATED, 1> : (MxFn)fq_mx_quantize_kernel<T, false, GATED, G>;
 }
@@ -510,23 +505,30 @@ static fq_status_t launch_mx(MxFn fn, MxParams& p, uint32_t G, void* stream) {
 }
 
 typedef void (*NormFn)(const NormParams);
-// `tpr`: threads to a row, `v`: vectors of eight to a thread
+// `tpr`: threads to a row, `v`: vectors of eight to a thread.  Two, which halves what a thread spends on the sums over the row (4096 rows
+// of 4096 50 us, with one 61); but one where every row has an SM to itself and only latency counts.
 template <class T, int FORMAT>
-static NormFn pick_norm(uint32_t D, uint32_t& tpr, uint32_t& v) {
+static NormFn pick_norm(uint32_t D, bool few, uint32_t& tpr, uint32_t& v) {
     const uint32_t vectors = (D + 7) / 8;
-    v = 1;
-    if (vectors <= 64) return tpr = 32, v = 2, (NormFn)fq_norm_kernel<T, 32, 2, FORMAT>;
-    if (vectors <= 128) return tpr = 128, (NormFn)fq_norm_kernel<T, 128, 1, FORMAT>;
-    if (vectors <= 256) return tpr = 256, (NormFn)fq_norm_kernel<T, 256, 1, FORMAT>;
-    if (vectors <= 512) return tpr = 512, (NormFn)fq_norm_kernel<T, 512, 1, FORMAT>;
-    if (vectors <= 1024) return tpr = 1024, (NormFn)fq_norm_kernel<T, 1024, 1, FORMAT>;
-    return tpr = 1024, v = 2, (NormFn)fq_norm_kernel<T, 1024, 2, FORMAT>;
+    if (few) {
+        v = 1;
+        if (vectors <= 128) return tpr = 128, (NormFn)fq_norm_kernel<T, 128, 1, FORMAT>;
+        if (vectors <= 256) return tpr = 256, (NormFn)fq_norm_kernel<T, 256, 1, FORMAT>;
+        if (vectors <= 512) return tpr = 512, (NormFn)fq_norm_kernel<T, 512, 1, FORMAT>;
+        if (vectors <= 1024) return tpr = 1024, (NormFn)fq_norm_kernel<T, 1024, 1, FORMAT>;
+    }
+    v = 2;
+    if (vectors <= 64) return tpr = 32, (NormFn)fq_norm_kernel<T, 32, 2, FORMAT>;
+    if (vectors <= 256) return tpr = 128, (NormFn)fq_norm_kernel<T, 128, 2, FORMAT>;
+    if (vectors <= 512) return tpr = 256, (NormFn)fq_norm_kernel<T, 256, 2, FORMAT>;
+    if (vectors <= 1024) return tpr = 512, (NormFn)fq_norm_kernel<T, 512, 2, FORMAT>;
+    return tpr = 1024, (NormFn)fq_norm_kernel<T, 1024, 2, FORMAT>;
 }
 template <class T>
-static NormFn pick_norm(int format, uint32_t D, uint32_t& tpr, uint32_t& v) {
-    if (format == (int)FQ_MXFP4) return pick_norm<T, (int)FQ_MXFP4>(D, tpr, v);
-    if (format == (int)FQ_NVFP4) return pick_norm<T, (int)FQ_NVFP4>(D, tpr, v);
-    return pick_norm<T, 2>(D, tpr, v);
+static NormFn pick_norm(int format, uint32_t D, bool few, uint32_t& tpr, uint32_t& v) {
+    if (format == (int)FQ_MXFP4) return pick_norm<T, (int)FQ_MXFP4>(D, few, tpr, v);
+    if (format == (int)FQ_NVFP4) return pick_norm<T, (int)FQ_NVFP4>(D, few, tpr, v);
+    return pick_norm<T, 2>(D, few, tpr, v);
 }
 // CTAs of a persistent kernel that fit on an SM, asked once per kernel (all devices are alike: sm_100a).
 static int ctas_per_sm(const void* fn, int threads, size_t smem) {
@@ -655,7 +657,7 @@ fq_status_t fq_mx_quantize_swiglu(const fq_mx_layout_t* L, const void* gate, uin
     p.a = gate, p.ld_a = ld_gate, p.b = up, p.ld_b = ld_up, p.codes = (uint32_t*)codes, p.scales = (uint8_t*)scales;
     p.lie = std::min(rows_lie(gate, ld_gate, 2, L->rows), rows_lie(up, ld_up, 2, L->rows));
     const bool nv = L->format == FQ_NVFP4, one = one_row_tasks(p, sm_count_cached());
-    return launch_mx(type == FQ_TYPE_BF16 ? pick_quantize<__nv_bfloat16, true>(nv, one) : pick_quantize<__half, true>(nv, one), p, one ? 1 : 2, cuda_stream);
+    return launch_mx(type == FQ_TYPE_BF16 ? pick_quantize<__nv_bfloat16, true>(nv, one) : pick_quantize<__half, true>(nv, one), p, 1, cuda_stream);
 }
 
 fq_status_t fq_mx_dequantize(const fq_mx_layout_t* L, const void* codes, const void* scales, const float* tensor_scale, void* Y,
@@ -728,7 +730,8 @@ fq_status_t fq_norm_block(const fq_norm_args_t* a, void* cuda_stream) {
     const int sms = sm_count_cached();
     if (sms <= 0) return fail(FQ_ERR_CUDA, "no CUDA device: %s", cudaGetErrorString(cudaGetLastError()));
     uint32_t tpr = 0, v = 0;
-    const NormFn fn = a->type == FQ_TYPE_BF16 ? pick_norm<__nv_bfloat16>(format, a->D, tpr, v) : pick_norm<__half>(format, a->D, tpr, v);
+    const bool few = a->rows <= (uint32_t)sms;
+    const NormFn fn = a->type == FQ_TYPE_BF16 ? pick_norm<__nv_bfloat16>(format, a->D, few, tpr, v) : pick_norm<__half>(format, a->D, few, tpr, v);
     const uint32_t threads = std::max<uint32_t>(tpr, 128), per = threads / tpr, smem = 48 * v * threads;
     const cudaError_t e = ensure_smem_attr((const void*)fn, (int)smem);
     if (e != cudaSuccess) return fail(FQ_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));

@@ -185,7 +185,7 @@ def test_norm_block(D, post, gate, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP16])
-@pytest.mark.parametrize("rows,D", [(1, 4096), (129, 256), (200, 160), (260, 1056)])
+@pytest.mark.parametrize("rows,D", [(1, 4096), (129, 256), (200, 160), (260, 1056), (150, 2976), (151, 4096), (149, 8192), (160, 32)])
 def test_norm_block_many_rows_and_strides(rows, D, dtype):
     g = torch.Generator().manual_seed(rows)
     x, o = torch.randn(rows, D, generator=g).to(dtype), torch.randn(rows, D, generator=g).to(dtype)
