@@ -499,9 +499,11 @@ static MxFn pick_dequantize(bool nv, bool one) {
 static fq_status_t launch_mx(MxFn fn, MxParams& p, uint32_t G, void* stream) {
     // lines of tasks: the first 32 rows of each 32 G (rows 32 further on go with them)
     p.tasks = ((uint64_t)(p.rows / (32 * G)) * 32 + std::min<uint32_t>(p.rows % (32 * G), 32)) * p.chunks;
-    const uint64_t warps = kMxThreads / 32, ctas = (p.tasks + warps - 1) / warps;
+    // (few warps: CTAs of two, so that they are spread over the SMs)
+    const uint32_t threads = p.tasks <= 32ull * sm_count_cached() ? 64 : kMxThreads;
+    const uint64_t warps = threads / 32, ctas = (p.tasks + warps - 1) / warps;
     if (ctas > 0x7fffffffull) return fail(FQ_ERR_UNSUPPORTED_SHAPE, "matrix too large for one launch");
-    return launch(fn, dim3((uint32_t)ctas), kMxThreads, 0, 1, stream, p);
+    return launch(fn, dim3((uint32_t)ctas), threads, 0, 1, stream, p);
 }
 
 typedef void (*NormFn)(const NormParams);
@@ -583,15 +585,60 @@ static fq_status_t launch_mx_gemm(const fq_mx_layout_t* LX, const void* xc, cons
     if (tiles > 0x7fffffffull) return fail(FQ_ERR_UNSUPPORTED_SHAPE, "too many tiles");
     p.tiles = (uint32_t)tiles;
     p.steps = (p.K + kMxStageK - 1) / kMxStageK;
-    p.stages = G::STAGES < 16 ? G::STAGES : 16;
+    // The steps of a tile over up to eight CTAs.  The first halving costs an exchange of about a microsecond (more tokens: two), each
+    // halving saves 0.18 us for each step of a CTA that it takes away, and CTAs that share an SM, or wait for one, lose it again.
+    // So: from 16 steps (more than 32 tokens: 32) while a CTA has 8 (16), on as many CTAs as there are SMs, or twice that where the tile is
+    // already split.  us for 1, 2, 4, 8 CTAs: 8 steps, 64 tiles, one token 4.2, 4.7, 4.8, 9.4; 16 steps, 32 tiles 6.2, 5.5, 4.75, 5.1, 64 tokens
+    // 6.0, 6.4, 7.0, 8.2; 56 steps, 32 tiles 14.3, 10.5, 9.4, 8.8, 64 tokens 14.7, 11.4, 10.7, 12.0; 12 steps, 87 tiles 6.8, 7.8, 11, 16.
+    constexpr uint32_t least = NT <= 32 ? 8 : 16;
     p.split = 1;
-    while (p.split < 8 && p.tiles * p.split * 2 <= sms && p.steps >= 4 * p.split) p.split *= 2;
-    const uint32_t grid = p.split > 1 ? p.tiles * p.split : std::min(p.tiles, sms);
+    while (p.split < 8 && p.steps >= 2 * least && p.steps >= least * p.split &&
+           p.tiles * p.split * 2 <= (NT <= 32 && p.split > 1 ? 2 * sms : sms))
+        p.split *= 2;
+    const uint32_t grid = p.split > 1 ? p.tiles * p.split : std::min(p.tiles, 2 * sms);
+    // a CTA that has its SM to itself, and more steps than the shorter ring holds, gets all of the shared memory (4096 x 4096, 128 tokens:
+    // three stages 8.3 us, six 6.3; 11133 x 2976, 77 tokens, 12.0 and 9.9)
+    p.stages = std::min(grid <= sms && (p.steps + p.split - 1) / p.split > G::STAGES ? G::STAGES_ALONE : G::STAGES, kMxStages);
     const auto fn = fq_mx_gemm_kernel<T, NT, NV>;
+    const uint32_t smem = p.stages * G::STAGE + 1024;
+    const cudaError_t e = ensure_smem_attr((const void*)fn, (int)(std::min(G::STAGES_ALONE, kMxStages) * G::STAGE + 1024));
+    if (e != cudaSuccess) return fail(FQ_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
+    return launch(fn, dim3(grid), G::THREADS, smem, p.split, stream, mw, mx, mws, mxs, p);
+}
+template <class T, bool NV>
+static fq_status_t launch_mx_pair(const fq_mx_layout_t* LX, const void* xc, const void* xs, const fq_mx_layout_t* LW, const void* wc, const void* ws,
+                                  const MxGemmParams& g, uint32_t tokens, uint32_t sms, void* stream) {
+    using G = MxPair<NV>;
+    const EncodeFn enc = tensor_map_encoder();
+    if (!enc) return fail(FQ_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
+    CUtensorMap mw, mx, mws, mxs;
+    fq_status_t st;
+    if ((st = encode_codes(enc, LW, wc, 128, &mw)) != FQ_OK || (st = encode_codes(enc, LX, xc, tokens / 2, &mx)) != FQ_OK ||
+        (st = encode_scales(enc, LW, ws, G::ATOMS, 1, &mws)) != FQ_OK || (st = encode_scales(enc, LX, xs, G::ATOMS, tokens / 128, &mxs)) != FQ_OK)
+        return st;
+    MxPairParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.Y = g.Y, p.ldy = g.ldy, p.ts_x = g.ts_x, p.ts_w = g.ts_w, p.status = g.status, p.M = g.M, p.N = g.N, p.K = g.K;
+    p.tokens = tokens;
+    p.tiles_m = (p.M + tokens - 1) / tokens;
+    const uint64_t tiles = (uint64_t)p.tiles_m * ((p.N + 255) / 256);
+    if (tiles > 0x7fffffffull) return fail(FQ_ERR_UNSUPPORTED_SHAPE, "too many tiles");
+    p.tiles = (uint32_t)tiles;
+    p.steps = (p.K + kMxStageK - 1) / kMxStageK;
+    p.stages = G::STAGES < 8 ? G::STAGES : 8;
+    const auto fn = fq_mx_pair_kernel<T, NV>;
     const uint32_t smem = p.stages * G::STAGE + 1024;
     const cudaError_t e = ensure_smem_attr((const void*)fn, (int)smem);
     if (e != cudaSuccess) return fail(FQ_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
-    return launch(fn, dim3(grid), 256, smem, p.split, stream, mw, mx, mws, mxs, p);
+    return launch(fn, dim3(2 * std::min(p.tiles, sms / 2)), 32 * kPairWarps, smem, 1, stream, mw, mx, mws, mxs, p);
+}
+// Tokens of a tile of the pair kernel: 256, unless tiles of 128 leave the busiest pair less to do.
+static uint32_t pair_tokens(uint32_t M, uint32_t N, uint32_t sms) {
+    auto work = [&](uint32_t t) {
+        const uint64_t tiles = (uint64_t)((M + t - 1) / t) * ((N + 255) / 256), pairs = sms / 2;
+        return (tiles + pairs - 1) / pairs * t;
+    };
+    return work(128) < work(256) ? 128 : 256;
 }
 template <class T, bool NV>
 static fq_status_t launch_mx_gemm(const fq_mx_layout_t* LX, const void* xc, const void* xs, const fq_mx_layout_t* LW, const void* wc, const void* ws,
@@ -599,6 +646,7 @@ static fq_status_t launch_mx_gemm(const fq_mx_layout_t* LX, const void* xc, cons
     if (p.M <= 16) return launch_mx_gemm<T, 16, NV>(LX, xc, xs, LW, wc, ws, p, sms, stream);
     if (p.M <= 32) return launch_mx_gemm<T, 32, NV>(LX, xc, xs, LW, wc, ws, p, sms, stream);
     if (p.M <= 64) return launch_mx_gemm<T, 64, NV>(LX, xc, xs, LW, wc, ws, p, sms, stream);
+    if (p.M > 128 && sms >= 2) return launch_mx_pair<T, NV>(LX, xc, xs, LW, wc, ws, p, pair_tokens(p.M, p.N, sms), sms, stream);
     return launch_mx_gemm<T, 128, NV>(LX, xc, xs, LW, wc, ws, p, sms, stream);
 }
 
