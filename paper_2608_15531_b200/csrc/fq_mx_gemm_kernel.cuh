@@ -165,7 +165,8 @@ fq_mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
     __shared__ uint32_t tmem_slot;
     __shared__ uint32_t abort_word;
     namespace cg = cooperative_groups;
-    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31, S = p.stages;
+    // (the shuffle tells the compiler that a warp's lanes agree: the tensor warp's operands then stay in uniform registers)
+    const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31, S = p.stages;
     const uint32_t smem = (smem_u32(mx_smem) + 1023) & ~1023u;
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * kMxStages, bar_acc = bar_empty + 8 * kMxStages, bar_free = bar_acc + 8 * G::ACCS, bar_final = bar_free + 8 * G::ACCS;
     volatile uint32_t* abort_flag = &abort_word;
@@ -377,8 +378,10 @@ __device__ __forceinline__ void pair_load_3d(uint32_t dst, const CUtensorMap* ma
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
+// What it tells of is a read of tensor memory that has been waited for; nothing in memory goes with it, so that it need not wait for the
+// thread's stores to Y (as a release it took 1900 clocks, a tenth of a tile of 4096 k).
 __device__ __forceinline__ void arrive_remote(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 template <class T, bool NV>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * kPairWarps, 1)
@@ -391,7 +394,8 @@ fq_mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
     __shared__ uint32_t abort_word;
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
-    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31, S = p.stages, rank = blockIdx.x & 1;
+    // (the shuffle tells the compiler that a warp's lanes agree: the tensor warp's operands then stay in uniform registers)
+    const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31, S = p.stages, rank = blockIdx.x & 1;
     const uint32_t smem = (smem_u32(mx_smem) + 1023) & ~1023u;
     // full: the leader's, for the copies of both CTAs; empty, acc, final: each CTA's own, by commits to both; free: the leader's
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 64, bar_acc = bar_empty + 64, bar_free = bar_acc + 8, bar_final = bar_free + 8;
