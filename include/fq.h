@@ -354,7 +354,7 @@ fq_status_t fq_fused_host_io_async(const fq_layout_t* L, const void* X_host, uin
  *              amax > 0; d = s ts rounded to binary32
  *   code       e2m1(x / d) of the exact quotient, rounded to nearest even, at most 6 in magnitude
  * A block that holds a NaN or an infinity gets the scale NaN and codes 0: it reads back as NaN.  A tensor scale that is
- * not in [2^-100, 2^100] gives NaN scales throughout.
+ * not in [2^-60, 2^60] gives NaN scales throughout.
  *
  * Stored form of a rows x K matrix (K a multiple of 32):
  *   codes    rows x K/2 bytes, row-major, value k in nibble k % 2 of byte k / 2 (even k: low nibble)

@@ -194,7 +194,7 @@ __device__ __forceinline__ float e4m3_value(uint32_t b) {
 __device__ __forceinline__ float e2m1_value(uint32_t c) {                                  // of the three lower bits
     return c & 6 ? __uint_as_float(((c & 7) << 22) + (126u << 23)) : 0.5f * (float)(c & 1);
 }
-constexpr float kMinTensorScale = 0x1p-100f, kMaxTensorScale = 0x1p100f;
+constexpr float kMinTensorScale = 0x1p-60f, kMaxTensorScale = 0x1p60f;       // (the product of two is a normal number)
 
 // The tensor's part of an FQ_NVFP4 quantisation.
 struct TensorScale {

@@ -219,6 +219,7 @@ fq_mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
         }
         let_copies_land(bar_full, issued, S);             // (at once, unless another warp gives up)
     } else if (warp == 1) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");     // (its waits are limited in time, the grid before is not)
         // e2m1 times e2m1, scales E8M0 (bit 23) or E4M3, N = NT, M = 128
         StageWork w;
         w.idesc = (1u << 7) | (1u << 10) | ((uint32_t)(NT >> 3) << 17) | (NV ? 0u : 1u << 23) | (8u << 24);
@@ -448,6 +449,7 @@ fq_mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
         for (uint32_t j = (issued > S ? issued - S : 0); j < issued; ++j) mbar_wait_leaving(bar_empty + 8 * (j % S), (j / S) & 1);
     } else if (warp == 1) {
         if (rank == 0) {
+            asm volatile("griddepcontrol.wait;" ::: "memory");     // (its waits are limited in time, the grid before is not)
             // e2m1 times e2m1, scales E8M0 (bit 23) or E4M3, M = 256
             const uint32_t idesc = (1u << 7) | (1u << 10) | (NV ? 0u : 1u << 23) | (16u << 24);
             StageWork w;

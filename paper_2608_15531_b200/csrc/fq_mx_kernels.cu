@@ -458,7 +458,7 @@ static bool disjoint(const Piece* out, int nout, const Piece* in, int nin) {
 }
 static fq_status_t check_stride(const char* what, const void* p, uint64_t rows, uint64_t cols, uint64_t ld, size_t size) {
     if (!aligned(p, size)) return fail(FQ_ERR_INVALID_ARG, "%s is misaligned", what);
-    if ((rows > 1 && ld < cols) || ld > (1ull << 40)) return fail(FQ_ERR_INVALID_ARG, "%s: row stride %llu for %llu columns", what, (unsigned long long)ld, (unsigned long long)cols);
+    if ((rows > 1 && ld < cols) || ld > (1ull << 40) || (rows - 1) > (1ull << 56) / (ld + 1)) return fail(FQ_ERR_INVALID_ARG, "%s: row stride %llu for %llu columns", what, (unsigned long long)ld, (unsigned long long)cols);
     return FQ_OK;
 }
 static fq_status_t check_mx(const fq_mx_layout_t* L, const void* codes, const void* scales, const float* ts) {
@@ -590,15 +590,18 @@ static fq_status_t launch_mx_gemm(const fq_mx_layout_t* LX, const void* xc, cons
     // So: from 16 steps (more than 32 tokens: 32) while a CTA has 8 (16), on as many CTAs as there are SMs, or twice that where the tile is
     // already split.  us for 1, 2, 4, 8 CTAs: 8 steps, 64 tiles, one token 4.2, 4.7, 4.8, 9.4; 16 steps, 32 tiles 6.2, 5.5, 4.75, 5.1, 64 tokens
     // 6.0, 6.4, 7.0, 8.2; 56 steps, 32 tiles 14.3, 10.5, 9.4, 8.8, 64 tokens 14.7, 11.4, 10.7, 12.0; 12 steps, 87 tiles 6.8, 7.8, 11, 16.
+    // Clusters of four and eight do not fill every group of SMs: an eighth is left out of the count (34 tiles of eight CTAs, two to
+    // an SM, 10.1 us, of four 6.6; 36 tiles of four with an SM to each 10 us, 33 of them 6.6).
     constexpr uint32_t least = NT <= 32 ? 8 : 16;
+    const uint32_t most = sms - sms / 8;
     p.split = 1;
     while (p.split < 8 && p.steps >= 2 * least && p.steps >= least * p.split &&
-           p.tiles * p.split * 2 <= (NT <= 32 && p.split > 1 ? 2 * sms : sms))
+           p.tiles * p.split * 2 <= (p.split == 1 ? sms : (NT <= 32 ? 2 : 1) * most))
         p.split *= 2;
     const uint32_t grid = p.split > 1 ? p.tiles * p.split : std::min(p.tiles, 2 * sms);
     // a CTA that has its SM to itself, and more steps than the shorter ring holds, gets all of the shared memory (4096 x 4096, 128 tokens:
     // three stages 8.3 us, six 6.3; 11133 x 2976, 77 tokens, 12.0 and 9.9)
-    p.stages = std::min(grid <= sms && (p.steps + p.split - 1) / p.split > G::STAGES ? G::STAGES_ALONE : G::STAGES, kMxStages);
+    p.stages = std::min(grid <= (p.split > 2 ? most : sms) && (p.steps + p.split - 1) / p.split > G::STAGES ? G::STAGES_ALONE : G::STAGES, kMxStages);
     const auto fn = fq_mx_gemm_kernel<T, NT, NV>;
     const uint32_t smem = p.stages * G::STAGE + 1024;
     const cudaError_t e = ensure_smem_attr((const void*)fn, (int)(std::min(G::STAGES_ALONE, kMxStages) * G::STAGE + 1024));

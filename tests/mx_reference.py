@@ -35,7 +35,7 @@ def quantize(x, fmt, ts=1.0):
             byte = np.where(bad, 255, byte)
         else:
             ts32 = np.float32(ts)
-            if not (np.float32(2.0 ** -100) <= ts32 <= np.float32(2.0 ** 100)):
+            if not (np.float32(2.0 ** -60) <= ts32 <= np.float32(2.0 ** 60)):
                 bad = np.ones_like(bad)
                 ts32 = np.float32(1.0)
             byte = nearest(amax / (6.0 * np.float64(ts32)), E4M3)

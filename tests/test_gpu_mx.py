@@ -67,7 +67,7 @@ def test_quantize(rows, K, fmt, ts, dtype):
         assert R.same(y, R.round_to(R.values(*ref, fmt, 1.0 if ts is None else ts), out))
 
 
-@pytest.mark.parametrize("ts", [0.0, -1.0, float("nan"), float("inf"), 1e-35, 1e35])
+@pytest.mark.parametrize("ts", [0.0, -1.0, float("nan"), float("inf"), 2.0 ** -60.5, 2.0 ** 60.5])
 def test_a_tensor_scale_out_of_range_gives_nan(ts):
     L = fq.fq_mx_get_layout(3, 64, 1)
     codes, scales = buffers(L)
@@ -78,7 +78,7 @@ def test_a_tensor_scale_out_of_range_gives_nan(ts):
     assert bool(y.isnan().all())
 
 
-@pytest.mark.parametrize("ts", [2.0 ** -100, 2.0 ** 100, 1.5 * 2.0 ** -70])
+@pytest.mark.parametrize("ts", [2.0 ** -60, 2.0 ** 60, 1.5 * 2.0 ** -41])
 def test_tensor_scales_at_the_ends_of_their_range(ts):
     L = fq.fq_mx_get_layout(9, 96, 1)
     x = (torch.randn(9, 96, generator=torch.Generator().manual_seed(1)).double() * ts * 100).float()
@@ -351,6 +351,76 @@ def test_gemm_reads_what_the_call_before_it_wrote(ws):
             out.append(Y)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, got)) and not torch.equal(want[0], want[1])
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_offsets_beyond_32_bits(fmt, ws):
+    """Rows that lie 2^31 values apart: the third begins beyond 2^32 values, 8 GB from the first."""
+    rows, K, ld = 3, 96, 1 << 31
+    free, _ = torch.cuda.mem_get_info()
+    if free < 24 << 30:
+        pytest.skip("needs 24 GB of device memory")
+    L = fq.fq_mx_get_layout(rows, K, fmt)
+    x = hard_rows(rows, K, BF16, 9)
+    ref = R.quantize(R.f64(x), fmt)
+    wide = torch.empty(2 * ld + K + 64, dtype=BF16, device="cuda")
+    view = torch.as_strided(wide, (rows, K), (ld, 1))
+    view.copy_(x)
+    codes, scales = buffers(L)
+    fq.fq_mx_quantize(L, view, codes, scales)
+    check_stored(L, codes, scales, ref)
+    view.zero_()
+    fq.fq_mx_dequantize(L, codes, scales, view)
+    assert R.same(view, R.round_to(R.values(*ref, fmt), BF16))
+    fq.fq_mx_quantize_swiglu(L, view, torch.as_strided(wide, (rows, K), (ld, 1)), *buffers(L))
+    r, h = R.norm_block(R.f64(view), 1e-5)
+    fq.fq_norm_block(view, 1e-5, R=view, H=(out := torch.empty(rows, K, dtype=BF16, device="cuda")))
+    assert R.same(view, R.round_to(r, BF16)) and R.same(out, R.round_to(h, BF16))
+    rng = np.random.default_rng(0)
+    X, W = operand(rng, rows, K, fmt, True), operand(rng, 96, K, fmt, True)
+    fq.fq_mx_gemm(L, X[0], X[1], fq.fq_mx_get_layout(96, K, fmt), W[0], W[1], view, ws)
+    assert R.same(view, R.round_to(X[2] @ W[2].T, BF16))
+
+
+def test_gemm_tensor_scales_whose_product_is_small(ws):
+    """Scales of 2^-60 and 2^-59: their product is a normal number of FP32, and so are the results."""
+    rng = np.random.default_rng(8)
+    LX, LW = fq.fq_mx_get_layout(4, 64, 1), fq.fq_mx_get_layout(140, 64, 1)
+    x, w = operand(rng, 4, 64, 1, True), operand(rng, 140, 64, 1, True)
+    a, b = 2.0 ** -60, 2.0 ** -59
+    Y = product(LX, x, LW, w, FP32, ws, x_tensor_scale=scale_tensor(a), w_tensor_scale=scale_tensor(b))
+    assert R.same(Y, torch.from_numpy((x[2] @ w[2].T) * (a * b)))
+
+
+_CAPTURED_FIRST = """
+import torch
+from paper_2608_15531_b200 import binding as fq
+x = torch.randn(300, 512, device="cuda").bfloat16()
+L, W = fq.fq_mx_get_layout(300, 512, 0), fq.fq_mx_get_layout(300, 512, 0)
+c, s = (torch.zeros(n, dtype=torch.uint8, device="cuda") for n in fq.fq_mx_sizes(L))
+Y, H, ws = torch.empty(300, 300, device="cuda"), torch.empty_like(x), torch.zeros(fq.FQ_MX_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+def run():
+    fq.fq_norm_block(x, 1e-5, H=H, layout=L, codes=c, scales=s)
+    fq.fq_mx_gemm(L, c, s, W, c, s, Y, ws)
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    run()
+g.replay()
+torch.cuda.synchronize()
+first = Y.clone()
+run()
+fq.fq_check_status(ws)
+assert torch.equal(first, Y) and bool(Y.any())
+"""
+
+
+def test_the_first_calls_of_a_process_are_captured():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    p = subprocess.run([sys.executable, "-c", _CAPTURED_FIRST], cwd=root, capture_output=True, text=True)
+    assert p.returncode == 0, p.stderr[-800:]
 
 
 # --------------------------------------------------------------------------------------- a decoder's block, and captured
