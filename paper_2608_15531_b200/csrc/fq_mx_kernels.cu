@@ -601,7 +601,8 @@ static fq_status_t launch_mx_gemm(const fq_mx_layout_t* LX, const void* xc, cons
     const uint32_t grid = p.split > 1 ? p.tiles * p.split : std::min(p.tiles, 2 * sms);
     // a CTA that has its SM to itself, and more steps than the shorter ring holds, gets all of the shared memory (4096 x 4096, 128 tokens:
     // three stages 8.3 us, six 6.3; 11133 x 2976, 77 tokens, 12.0 and 9.9)
-    p.stages = std::min(grid <= (p.split > 2 ? most : sms) && (p.steps + p.split - 1) / p.split > G::STAGES ? G::STAGES_ALONE : G::STAGES, kMxStages);
+    const uint32_t alone = p.split == 8 ? sms - sms / 4 : p.split == 4 ? most : sms;
+    p.stages = std::min(grid <= alone && (p.steps + p.split - 1) / p.split > G::STAGES ? G::STAGES_ALONE : G::STAGES, kMxStages);
     const auto fn = fq_mx_gemm_kernel<T, NT, NV>;
     const uint32_t smem = p.stages * G::STAGE + 1024;
     const cudaError_t e = ensure_smem_attr((const void*)fn, (int)(std::min(G::STAGES_ALONE, kMxStages) * G::STAGE + 1024));
@@ -649,7 +650,10 @@ static fq_status_t launch_mx_gemm(const fq_mx_layout_t* LX, const void* xc, cons
     if (p.M <= 16) return launch_mx_gemm<T, 16, NV>(LX, xc, xs, LW, wc, ws, p, sms, stream);
     if (p.M <= 32) return launch_mx_gemm<T, 32, NV>(LX, xc, xs, LW, wc, ws, p, sms, stream);
     if (p.M <= 64) return launch_mx_gemm<T, 64, NV>(LX, xc, xs, LW, wc, ws, p, sms, stream);
-    if (p.M > 128 && sms >= 2) return launch_mx_pair<T, NV>(LX, xc, xs, LW, wc, ws, p, pair_tokens(p.M, p.N, sms), sms, stream);
+    // More than 128 tokens: single CTAs while each of their tiles has an SM (4096 x 4096, 512 tokens, 128 tiles, 6.6 us, pairs 7.5; 14336 x 4096,
+    // 256 tokens, 13.8 and 17.4), pairs beyond (4096 x 4096, 2048 tokens, 17.0 and 14.6; 4096 x 14336 58 and 42).
+    if (p.M > 128 && (uint64_t)((p.M + 127) / 128) * ((p.N + 127) / 128) > sms && sms >= 2)
+        return launch_mx_pair<T, NV>(LX, xc, xs, LW, wc, ws, p, pair_tokens(p.M, p.N, sms), sms, stream);
     return launch_mx_gemm<T, 128, NV>(LX, xc, xs, LW, wc, ws, p, sms, stream);
 }
 

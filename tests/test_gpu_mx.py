@@ -246,7 +246,7 @@ def ws():
 @pytest.mark.parametrize("fmt", [0, 1])
 @pytest.mark.parametrize("M,N,K", [(1, 1, 32), (1, 128, 64), (1, 129, 96), (2, 100, 160), (16, 256, 256), (17, 130, 288), (32, 127, 512), (33, 384, 544),
                                    (64, 200, 1024), (65, 129, 992), (100, 64, 2048), (128, 300, 320), (129, 257, 736), (300, 333, 1056), (520, 700, 416),
-                                   (1, 4096, 1024), (3, 513, 2048), (777, 130, 96), (1, 20000, 128), (1000, 2000, 64), (1011, 9400, 160), (1040, 9472, 544), (1160, 9300, 96)])
+                                   (1, 4096, 1024), (3, 513, 2048), (777, 130, 96), (1, 20000, 128), (1000, 2000, 64), (1011, 9400, 160), (1040, 9472, 544), (1160, 9300, 96), (129, 19200, 96), (150, 19300, 320)])
 def test_gemm_exact_sums(M, N, K, fmt, ws):
     """Products are multiples of 2^-4 of magnitude up to 144, and K of them below 2^18: each sum has at most 24 bits,
     in whatever order, so that the result is the exact one rounded once."""
@@ -262,7 +262,7 @@ def test_gemm_exact_sums(M, N, K, fmt, ws):
 
 
 @pytest.mark.parametrize("fmt", [0, 1])
-@pytest.mark.parametrize("M,N,K", [(1, 4096, 4096), (16, 4096, 14336), (77, 1133, 2976), (260, 1000, 4096)])
+@pytest.mark.parametrize("M,N,K", [(1, 4096, 4096), (16, 4096, 14336), (77, 1133, 2976), (260, 1000, 4096), (1100, 9500, 1056)])
 def test_gemm_general_scales(M, N, K, fmt, ws):
     """Sums that FP32 cannot hold.  Each of the K additions may be off by 2^-23 of the magnitudes summed (a truncated addition), the
     tensor scales' product and its multiplication by 2^-23 of the result, and the final rounding by half a step."""
@@ -296,7 +296,7 @@ def test_gemm_nan_scales_reach_their_rows_only(fmt, ws):
 
 def test_gemm_rows_of_y_with_a_stride(ws):
     rng = np.random.default_rng(2)
-    for M, N, K in ((5, 130, 128), (140, 260, 512)):
+    for M, N, K in ((5, 130, 128), (140, 260, 512), (1030, 9401, 64)):
         LX, LW = fq.fq_mx_get_layout(M, K, 0), fq.fq_mx_get_layout(N, K, 0)
         x, w = operand(rng, M, K, 0, True), operand(rng, N, K, 0, True)
         want = R.round_to(x[2] @ w[2].T, BF16)
@@ -309,9 +309,9 @@ def test_gemm_rows_of_y_with_a_stride(ws):
             assert bool((wide == 9.0).all())
 
 
-def test_gemm_is_reproducible_and_shares_its_workspace(ws):
+@pytest.mark.parametrize("M,N,K", [(8, 512, 8192), (1030, 9600, 288)])
+def test_gemm_is_reproducible_and_shares_its_workspace(M, N, K, ws):
     rng = np.random.default_rng(3)
-    M, N, K = 8, 512, 8192
     LX, LW = fq.fq_mx_get_layout(M, K, 1), fq.fq_mx_get_layout(N, K, 1)
     x, w = operand(rng, M, K, 1, False), operand(rng, N, K, 1, False)
     first = product(LX, x, LW, w, FP32, ws)
