@@ -128,46 +128,8 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
     asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-__device__ __forceinline__ uint32_t min_u16x2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("min.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-__device__ __forceinline__ uint32_t add_u16x2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("add.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-
-// Whether rounding `h` to T may come out differently from rounding the exact value, of which h is a binary32 result that is off by
-// less than U units in its last place: h is within U units of a border (the middle between two values of T), or so small that
-// borders lie elsewhere, or that the products on the way to h may have lost bits.
-template <class T> struct Border;
-template <> struct Border<__nv_bfloat16> {
-    static constexpr uint32_t SHIFT = 0, SMALL = 0x1780;                   // bits that rounding drops: 16; 2^-80
-};
-template <> struct Border<__half> {
-    static constexpr uint32_t SHIFT = 3, SMALL = 0x0401;                   // 13; just above the smallest normal number, 2^-14
-};
-template <uint32_t U, class T>
-__device__ __forceinline__ bool near_border(float h) {
-    using B = Border<T>;
-    const uint32_t low = (__float_as_uint(h) << B::SHIFT) + 0x8000u + (U << B::SHIFT);
-    const T r = from_float<T>(h);
-    return (low & 0xffffu) <= 2 * (U << B::SHIFT) || (*reinterpret_cast<const uint16_t*>(&r) & 0x7fffu) < B::SMALL;
-}
-// Of any of eight, `q` being their rounded values: two to an instruction.
-template <uint32_t U, class T>
-__device__ __forceinline__ bool near_border8(const float (&f)[8], const uint4& q) {
-    using B = Border<T>;
-    constexpr uint32_t add = (0x8000u + (U << B::SHIFT)) * 0x10001u;
-    uint32_t low = 0xffffffffu;
-#pragma unroll
-    for (int i = 0; i < 8; i += 2)
-        low = min_u16x2(low, add_u16x2(__byte_perm(__float_as_uint(f[i]) << B::SHIFT, __float_as_uint(f[i + 1]) << B::SHIFT, 0x5410), add));
-    uint32_t mag = min_u16x2(min_u16x2(q.x & 0x7fff7fffu, q.y & 0x7fff7fffu), min_u16x2(q.z & 0x7fff7fffu, q.w & 0x7fff7fffu));
-    return min(low & 0xffffu, low >> 16) <= 2 * (U << B::SHIFT) || min(mag & 0xffffu, mag >> 16) < B::SMALL;
-}
+template <class T> struct IsBf16 { static constexpr bool value = false; };
+template <> struct IsBf16<__nv_bfloat16> { static constexpr bool value = true; };
 
 // --------------------------------------------------------------------------------------------------- quantising
 

@@ -27,8 +27,8 @@ __device__ __forceinline__ void grid_start() {
 // ------------------------------------------------------------------------------------ quantising and reading back
 
 // A warp takes 512 consecutive values, 16 to a lane (32 bytes of a 16-bit type: one load), of G rows that are 32 apart.  With
-// G = 4 (two for gated products: registers) their scales share the 16-byte lines of an atom, and four loads are in flight; with
-// G = 1 a small matrix is spread over more warps.  16 values are a block of FQ_NVFP4, whose scale (a quotient and its rounding) is then
+// G = 4 their scales share the 16-byte lines of an atom, and four loads are in flight; with G = 1 a small matrix is spread over
+// more warps, and gated products, which are bound by instructions, keep to 64 registers.  16 values are a block of FQ_NVFP4, whose scale (a quotient and its rounding) is then
 // computed by one lane.
 struct MxParams {
     const void* a;               // X, or the gate
@@ -73,7 +73,7 @@ __device__ __forceinline__ float gated(float g, float u) {
 __device__ __noinline__ float gated_exact(float g, float u) { return (float)((double)g / (1.0 + exp(-(double)g)) * (double)u); }
 
 // A lane's 16 gated products, rounded to T and quantised.  The exact product lies between the computed one a little less and a little
-// more; where both round alike that is the result.  Where some do not (1 in 8192 values of BF16, 1 in 1024 of FP16), but
+// more; where both round alike that is the result.  Where some do not (1 in 3000 values of BF16, 1 in 400 of FP16), but
 // give the same codes and scales, no matter (h itself is not put out); else (one in some thousand warps) the warp takes what
 // is in question in binary64.  `again`: loads gate and up once more.
 template <class T, bool NV, class F>
@@ -89,12 +89,13 @@ __device__ __forceinline__ void quantize_gated16(const Words8& gate, const Words
         below += (hi.w[i] - pack2(a * (1.0f - E), b * (1.0f - E), T())) << i;
     }
     // the gate's bits as an unsigned number are above those of -80 where it is below -80 (or a NaN with a sign)
-    constexpr uint32_t deep = Border<T>::SHIFT ? 0xd500u : 0xc2a0u;
+    constexpr bool BF = IsBf16<T>::value;
+    constexpr uint32_t deep = BF ? 0xc2a0u : 0xd500u;
     const uint4 g0 = gate.half(0), g1 = gate.half(1);
     const uint32_t gm = max_u16x2(max_u16x2(max_u16x2(g0.x, g0.y), max_u16x2(g0.z, g0.w)), max_u16x2(max_u16x2(g1.x, g1.y), max_u16x2(g1.z, g1.w)));
     // products so small that binary32 may have lost bits on the way: only where a whole block is
     const uint32_t m = max_u16x2(max_magnitude(hi.half(0)), max_magnitude(hi.half(1)));
-    const bool all = max(gm & 0xffffu, gm >> 16) > deep || (!Border<T>::SHIFT && max(m & 0xffffu, m >> 16) < 0x1780u && m);
+    const bool all = max(gm & 0xffffu, gm >> 16) > deep || (BF && max(m & 0xffffu, m >> 16) < 0x1780u && m);
     quantize16<NV, T>(hi, ts, codes, scale);
     if (__any_sync(0xffffffffu, below != 0 || all)) {
         Words8 lo;
@@ -255,16 +256,18 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// CTAs to an SM that the registers have to allow: 768 threads (80 registers; with 512 4096 rows of 4096 take 55 us, with 768 50, with
-// 1024 67), one CTA where each is alone on its SM.
+// CTAs to an SM that the registers have to allow: 768 threads (80 registers; 4096 rows of 4096 with 512 threads 55 us, 768 50, 1024 67), one
+// CTA where each is alone on its SM.
 constexpr int norm_ctas(int tpr, int v) { return v == 1 || tpr >= 768 ? 1 : 768 / (tpr < 128 ? 128 : tpr); }
 
 // TPR threads to a row, V vectors of eight values to a thread, which stay in registers from the sum to the last store: one
 // pass over the data.  A CTA goes through rows; the next row's values are on their way to shared memory meanwhile (each
 // thread copies and reads its own, so that no barrier is needed).  Rows of up to 512 values share a CTA (TPR = 32, a warp to a row).
-// The residual sum and the sums of squares run in binary64 (the product of a weight and a gate is exact in binary32), and a result
-// of the second norm too near a border is taken in binary64: what is rounded is exact to about 2^-50.  Sums in binary32 would move a
-// value of H across a border in 1 of 10^4 cases, and a code of every tenth million by a step.
+// Sums and results run in binary64 (the product of a weight and a gate is exact in binary32).  In binary32 a value of H would
+// cross a border of its type in 1 of 10^4 cases, and a code of every tenth million be a step off; and B200 has the rate: 0.6
+// binary64 operations for each byte that a value moves.  What bounds it: 62 instructions a value, a third of them the sums
+// over a row and what a thread does once a row, 60 % of the issue slots at three rows to an SM (80 registers).  4096 rows of 4096, NVFP4 or
+// MXFP4, with a norm, a gate and everything put out 50 us (3.5 TB/s), without norm and gate 39; 2048 rows of 16384 99.
 template <class T, int TPR, int V, int FORMAT>                             // FORMAT: FQ_MXFP4, FQ_NVFP4, or 2 for none
 __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_ctas(TPR, V)) fq_norm_kernel(const NormParams p) {
     extern __shared__ uint4 ahead[];                       // [V][3][threads]: the next row's X, block and gate
@@ -370,7 +373,6 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_ctas(TPR, V)) fq_n
         }
         if (!p.h && FORMAT == 2) continue;
         const double rstd = rsqrt(fma(row_sum<TPR>(s[0] + s[1], part[2 + odd]), inv_d, (double)p.eps));
-        const float rs = (float)rstd;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const uint32_t c = column(j);
@@ -383,14 +385,8 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_ctas(TPR, V)) fq_n
                 for (int i = 0; i < 8; ++i) b[i] = 1.0f;
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = (float)r[j][i] * rs * b[i];  // off by two units at most: two conversions and two products
-            uint4 h = pack8<T>(f);
-            if (near_border8<4, T>(f, h)) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (near_border<4, T>(f[i])) f[i] = (float)(r[j][i] * rstd * (double)b[i]);
-                h = pack8<T>(f);
-            }
+            for (int i = 0; i < 8; ++i) f[i] = (float)(r[j][i] * rstd * (double)b[i]);
+            const uint4 h = pack8<T>(f);
             if (p.h && n > 0) store_raw((T*)p.h + row * p.ld_h + c, n, p.vec, h);
             if constexpr (FORMAT != 2) {
                 uint32_t codes, scale;
