@@ -16,6 +16,7 @@
 #include "fq_mx.cuh"
 #include "fq_mx_gemm_kernel.cuh"
 #include "fq_ptx.cuh"
+#include "fq_shares.h"
 
 namespace fq {
 
@@ -39,6 +40,7 @@ struct MxParams {
     uint8_t* scales;
     void* y;                     // (reading back)
     uint32_t rows, K, atoms, chunks;      // chunks of 512 values
+    Divisor by_chunks;
     uint64_t tasks;
     int lie;                     // RowsLie
 };
@@ -49,7 +51,7 @@ struct MxTask {
     __device__ __forceinline__ explicit MxTask(const MxParams& p) {
         const uint64_t w = (uint64_t)blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32;
         uint64_t line;
-        if ((p.tasks >> 32) == 0) line = (uint32_t)w / p.chunks;
+        if ((p.tasks >> 32) == 0) line = p.by_chunks((uint32_t)w);
         else line = w / p.chunks;
         any = w < p.tasks;
         row0 = G == 1 ? (uint32_t)line : (uint32_t)(line >> 5) * (32 * G) + (uint32_t)(line & 31);
@@ -120,7 +122,7 @@ __device__ __forceinline__ void quantize_gated16(const Words8& gate, const Words
 }
 
 template <class T, bool NV, bool GATED, int G>
-__global__ void __launch_bounds__(kMxThreads, GATED ? 4 : 1) fq_mx_quantize_kernel(const MxParams p) {
+__global__ void __launch_bounds__(kMxThreads, sizeof(T) == 2 ? (GATED || NV ? 4 : 5) : 1) fq_mx_quantize_kernel(const MxParams p) {
     const MxTask<G> task(p);
     grid_start();
     if (!task.any) return;
@@ -475,6 +477,7 @@ static MxParams mx_params(const fq_mx_layout_t* L, const float* ts) {
     p.ts = ts;
     p.rows = L->rows, p.K = L->K, p.atoms = mx_atoms(L);
     p.chunks = (L->K + 511) / 512;
+    p.by_chunks = Divisor::of(p.chunks);
     return p;
 }
 typedef void (*MxFn)(const MxParams);
