@@ -281,7 +281,7 @@ def fq_last_error() -> str:
 # ------------------------------------------------------------------ microscaled FP4
 #
 # X, Y, gate, ...: CUDA tensors of bfloat16, float16 or (quantize, dequantize, the product's Y) float32, two-dimensional, columns adjacent,
-# any row stride.  codes, scales: contiguous CUDA tensors of at least fq_mx_sizes(L) bytes.  tensor_scale: one float32
+# any row stride (a tensor of 16-bit patterns, as the INT4 calls take it, goes through .view(torch.bfloat16)).  codes, scales: contiguous CUDA tensors of at least fq_mx_sizes(L) bytes.  tensor_scale: one float32
 # value on the device (FQ_NVFP4; None means 1).  All on one device, which need not be the current one; the stream is the
 # given one or that device's current stream.
 
@@ -302,28 +302,38 @@ def fq_mx_sizes(L: MxLayout):
 
 def fq_mx_quantize(L: MxLayout, X, codes, scales, tensor_scale=None, stream=None) -> None:
     """Rows of values to codes and block scales."""
-    _check((_call or _pycall()).mx_quantize(L, X, codes, scales, tensor_scale, stream))
+    code = (_call or _pycall()).mx_quantize(L, X, codes, scales, tensor_scale, stream)
+    if code != FQ_OK:
+        _check(code)
 
 
 def fq_mx_quantize_swiglu(L: MxLayout, gate, up, codes, scales, tensor_scale=None, stream=None) -> None:
     """gate / (1 + exp(-gate)) * up, rounded to the inputs' type, to codes and block scales."""
-    _check((_call or _pycall()).mx_quantize_swiglu(L, gate, up, codes, scales, tensor_scale, stream))
+    code = (_call or _pycall()).mx_quantize_swiglu(L, gate, up, codes, scales, tensor_scale, stream)
+    if code != FQ_OK:
+        _check(code)
 
 
 def fq_mx_dequantize(L: MxLayout, codes, scales, Y, tensor_scale=None, stream=None) -> None:
     """The values that codes and scales stand for, in Y's type."""
-    _check((_call or _pycall()).mx_dequantize(L, codes, scales, Y, tensor_scale, stream))
+    code = (_call or _pycall()).mx_dequantize(L, codes, scales, Y, tensor_scale, stream)
+    if code != FQ_OK:
+        _check(code)
 
 
 def fq_mx_gemm(LX: MxLayout, x_codes, x_scales, LW: MxLayout, w_codes, w_scales, Y, workspace, x_tensor_scale=None,
                w_tensor_scale=None, stream=None) -> None:
     """Y (LX.rows x LW.rows) = x times w transposed.  workspace: FQ_MX_WORKSPACE_BYTES, zeroed once; fq_check_status reads it."""
-    _check((_call or _pycall()).mx_gemm(LX, x_codes, x_scales, x_tensor_scale, LW, w_codes, w_scales, w_tensor_scale, Y, workspace, stream))
+    code = (_call or _pycall()).mx_gemm(LX, x_codes, x_scales, x_tensor_scale, LW, w_codes, w_scales, w_tensor_scale, Y, workspace, stream)
+    if code != FQ_OK:
+        _check(code)
 
 
 def fq_norm_block(X, eps: float, *, block=None, block_weight=None, gate=None, residual_scale: float = 1.0, R=None, weight=None,
                   H=None, layout: MxLayout | None = None, codes=None, scales=None, tensor_scale=None, stream=None) -> None:
     """What stands between two blocks: R = X + residual_scale * gate * norm(block) (norm only with block_weight), H = norm(R) * weight,
     and H quantised (layout, codes, scales).  gate: as X, or one row for all rows.  R or H may be X or block (in place)."""
-    _check((_call or _pycall()).norm_block(X, eps, block, block_weight, gate, residual_scale, R, weight, H, layout, codes, scales,
-                                           tensor_scale, stream))
+    code = (_call or _pycall()).norm_block(X, eps, block, block_weight, gate, residual_scale, R, weight, H, layout, codes, scales,
+                                           tensor_scale, stream)
+    if code != FQ_OK:
+        _check(code)

@@ -14,6 +14,9 @@
 // Few tokens are bound by reading the weights once, and by latency on small layers: the k-steps of a tile are then split
 // over a cluster of CTAs, whose sums meet in shared memory and are added in rank order by all of them, each its tokens.
 // Tensor memory is given back before a CTA waits for its cluster, so that no CTA holds it while it waits for another one.
+// Measured (us, calls back to back in a graph, weights from DRAM): one token 4096 x 4096 4.5, 4096 x 28672 12.2 (5.1 TB/s), 14336 x 4096 NVFP4 8.5
+// (3.9); 128 tokens 5.8, 13.9, 11.9; 128 tokens 8192 x 57344 47 (5.7 TB/s, tensor pipe 35 % busy).  What bounds the small ones is the chain launch,
+// first copy, seven or fewer steps, tensor memory to registers, exchange, store: 3.7 us for 8 steps of 64 tiles.
 #pragma once
 #include <cooperative_groups.h>
 
@@ -65,8 +68,8 @@ __device__ __forceinline__ void tma_prefetch_2d(const CUtensorMap* map, uint32_t
 // A stage's work: its scales to tensor memory (one copy for each atom: 32 rows of 16 bytes, to the same lanes of each of the four
 // subpartitions), then D (+)= A B for each 64 of its 256 k.  tcgen05.cp and tcgen05.mma of one thread run in the order of their issue.
 // Whole warp, converged, with warp-uniform operands; one elected lane issues.  One asm block, so that the address arithmetic
-// is not in a divergent branch, where each operand has to be moved into a uniform register (4096 x 4096 x 28672: 273 us that
-// way, see the figure at the kernel for this one).
+// is not in a divergent branch, where each operand has to be moved into a uniform register: 440 clocks a stage of the pair kernel
+// went to its issue, now 245, and the loop around it took 270, now 100 (4096 x 4096 x 28672 238 us, now 197).
 //   cw, cx     tensor-memory columns of the two matrices' scales, multiples of four: an MMA whose scales begin in another
 //              column ends in an address error
 //   ws, xs     lower words of the descriptors of their atoms in shared memory, s_hi the upper word
@@ -343,6 +346,10 @@ fq_mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
 // sums into registers, all at once, give the columns back, and convert and store while the next tile is multiplied.
 // Tiles begin on multiples of 128 tokens, as the atoms of scales do; the last tile of a column multiplies only the tokens that it has,
 // rounded up to 32.
+// What bounds it: of the 12500 clocks of a tile of 4096 k the MMAs need 8200 (tensor pipe 68 % busy); 1700 pass between a tile's last
+// MMA and the next one's first (commit, tensor memory to registers, arrival from the other CTA), the rest waits for copies: six
+// stages of 35 KB are all the shared memory, and the L2 delivers 13 TB/s.  4096 x 4096 x 28672 197 us on one set of operands (4.9 PFLOP/s), 219 on
+// three in turn; 1024 x 4096 x 18944 29 (5.4 PFLOP/s).  Copies of the next tile's weights to the L2 ahead of time changed nothing.
 constexpr uint32_t kPairWarps = 12;        // copies, MMAs, allocation, one idle; eight drain warps: two for each 32 features
 
 struct MxPairParams {

@@ -1,5 +1,5 @@
 // Microscaled FP4 (sm_100a): quantising rows, also of a gated product or of the norm between two blocks, reading them back, and
-// the launchers of these kernels and of the product (fq_mx_gemm_kernel.cuh).
+// the launchers of these kernels and of the product (fq_mx_gemm_kernel.cuh).  The formats stand in fq.h.
 //
 // Every kernel is launched so that it may become resident while the grid before it drains (programmatic dependent
 // launch), and executes griddepcontrol.wait before it reads or writes global memory: any array may come from that grid.
@@ -31,6 +31,9 @@ __device__ __forceinline__ void grid_start() {
 // G = 4 their scales share the 16-byte lines of an atom, and four loads are in flight; with G = 1 a small matrix is spread over
 // more warps, and gated products, which are bound by instructions, keep to 64 registers.  16 values are a block of FQ_NVFP4, whose scale (a quotient and its rounding) is then
 // computed by one lane.
+// Measured (28672 x 4096 of BF16): MXFP4 45.6 us (6.5 TB/s, the rate of a copy), reading back 46.4; NVFP4 56.3 (5.3 TB/s: 11.8 instructions a
+// value, each rounded twice to see whether the quotient is near a border, 65 % of the issue slots).  Gated products, 4096 x 14336: 69 us (MXFP4, BF16;
+// 30 instructions a value, 72 % of the issue slots, and two of them on the quarter-rate pipe) and 89.5 (NVFP4, FP16; 42).
 struct MxParams {
     const void* a;               // X, or the gate
     const void* b;               // up
@@ -43,6 +46,7 @@ struct MxParams {
     Divisor by_chunks;
     uint64_t tasks;
     int lie;                     // RowsLie
+    uint32_t sms;
 };
 template <int G>
 struct MxTask {
@@ -266,10 +270,10 @@ constexpr int norm_ctas(int tpr, int v) { return v == 1 || tpr >= 768 ? 1 : 768 
 // pass over the data.  A CTA goes through rows; the next row's values are on their way to shared memory meanwhile (each
 // thread copies and reads its own, so that no barrier is needed).  Rows of up to 512 values share a CTA (TPR = 32, a warp to a row).
 // Sums and results run in binary64 (the product of a weight and a gate is exact in binary32).  In binary32 a value of H would
-// cross a border of its type in 1 of 10^4 cases, and a code of every tenth million be a step off; and B200 has the rate: 0.6
-// binary64 operations for each byte that a value moves.  What bounds it: 62 instructions a value, a third of them the sums
-// over a row and what a thread does once a row, 60 % of the issue slots at three rows to an SM (80 registers).  4096 rows of 4096, NVFP4 or
-// MXFP4, with a norm, a gate and everything put out 50 us (3.5 TB/s), without norm and gate 39; 2048 rows of 16384 99.
+// cross a border of its type in 1 of 10^4 cases, and a code of every tenth million be a step off.  What bounds it: 60 instructions
+// a value, half of them the sums over a row and what else a thread does once a row, on 59 % of the issue slots at three rows to an SM (80
+// registers); six conversions a value from and to binary64 keep their pipe 50 % busy.  4096 rows of 4096, with a norm behind the block, a gate
+// and everything put out 50 us (3.5 TB/s), without norm and gate 39; 2048 rows of 16384 99.
 template <class T, int TPR, int V, int FORMAT>                             // FORMAT: FQ_MXFP4, FQ_NVFP4, or 2 for none
 __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_ctas(TPR, V)) fq_norm_kernel(const NormParams p) {
     extern __shared__ uint4 ahead[];                       // [V][3][threads]: the next row's X, block and gate
@@ -478,11 +482,12 @@ static MxParams mx_params(const fq_mx_layout_t* L, const float* ts) {
     p.rows = L->rows, p.K = L->K, p.atoms = mx_atoms(L);
     p.chunks = (L->K + 511) / 512;
     p.by_chunks = Divisor::of(p.chunks);
+    p.sms = (uint32_t)std::max(sm_count_cached(), 1);      // (without a device the launch reports it)
     return p;
 }
 typedef void (*MxFn)(const MxParams);
 // Rows that a warp takes: four, unless that leaves SMs without a warp.
-static bool one_row_tasks(const MxParams& p, uint32_t sms) { return (uint64_t)p.rows * p.chunks <= 32ull * sms; }
+static bool one_row_tasks(const MxParams& p) { return (uint64_t)p.rows * p.chunks <= 32ull * p.sms; }
 template <class T, bool GATED>
 static MxFn pick_quantize(bool nv, bool one) {
     constexpr int G = GATED ? 1 : 4;
@@ -499,7 +504,7 @@ static fq_status_t launch_mx(MxFn fn, MxParams& p, uint32_t G, void* stream) {
     // lines of tasks: the first 32 rows of each 32 G (rows 32 further on go with them)
     p.tasks = ((uint64_t)(p.rows / (32 * G)) * 32 + std::min<uint32_t>(p.rows % (32 * G), 32)) * p.chunks;
     // (few warps: CTAs of two, so that they are spread over the SMs)
-    const uint32_t threads = p.tasks <= 32ull * sm_count_cached() ? 64 : kMxThreads;
+    const uint32_t threads = p.tasks <= 32ull * p.sms ? 64 : kMxThreads;
     const uint64_t warps = threads / 32, ctas = (p.tasks + warps - 1) / warps;
     if (ctas > 0x7fffffffull) return fail(FQ_ERR_UNSUPPORTED_SHAPE, "matrix too large for one launch");
     return launch(fn, dim3((uint32_t)ctas), threads, 0, 1, stream, p);
@@ -692,7 +697,7 @@ fq_status_t fq_mx_quantize(const fq_mx_layout_t* L, const void* X, uint32_t type
     MxParams p = mx_params(L, tensor_scale);
     p.a = X, p.ld_a = ldx, p.codes = (uint32_t*)codes, p.scales = (uint8_t*)scales;
     p.lie = rows_lie(X, ldx, size, L->rows);
-    const bool nv = L->format == FQ_NVFP4, one = one_row_tasks(p, sm_count_cached());
+    const bool nv = L->format == FQ_NVFP4, one = one_row_tasks(p);
     return launch_mx(type == FQ_TYPE_BF16 ? pick_quantize<__nv_bfloat16, false>(nv, one) : type == FQ_TYPE_FP16 ? pick_quantize<__half, false>(nv, one)
                                                                                                                : pick_quantize<float, false>(nv, one), p, one ? 1 : 4, cuda_stream);
 }
@@ -710,7 +715,7 @@ fq_status_t fq_mx_quantize_swiglu(const fq_mx_layout_t* L, const void* gate, uin
     MxParams p = mx_params(L, tensor_scale);
     p.a = gate, p.ld_a = ld_gate, p.b = up, p.ld_b = ld_up, p.codes = (uint32_t*)codes, p.scales = (uint8_t*)scales;
     p.lie = std::min(rows_lie(gate, ld_gate, 2, L->rows), rows_lie(up, ld_up, 2, L->rows));
-    const bool nv = L->format == FQ_NVFP4, one = one_row_tasks(p, sm_count_cached());
+    const bool nv = L->format == FQ_NVFP4, one = one_row_tasks(p);
     return launch_mx(type == FQ_TYPE_BF16 ? pick_quantize<__nv_bfloat16, true>(nv, one) : pick_quantize<__half, true>(nv, one), p, 1, cuda_stream);
 }
 
@@ -727,7 +732,7 @@ fq_status_t fq_mx_dequantize(const fq_mx_layout_t* L, const void* codes, const v
     MxParams p = mx_params(L, tensor_scale);
     p.y = Y, p.ld_a = ldy, p.codes = (uint32_t*)codes, p.scales = (uint8_t*)scales;      // (read)
     p.lie = rows_lie(Y, ldy, size, L->rows);
-    const bool nv = L->format == FQ_NVFP4, one = one_row_tasks(p, sm_count_cached());
+    const bool nv = L->format == FQ_NVFP4, one = one_row_tasks(p);
     return launch_mx(type == FQ_TYPE_BF16 ? pick_dequantize<__nv_bfloat16>(nv, one) : type == FQ_TYPE_FP16 ? pick_dequantize<__half>(nv, one)
                                                                                                           : pick_dequantize<float>(nv, one), p, one ? 1 : 4, cuda_stream);
 }

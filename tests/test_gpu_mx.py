@@ -294,6 +294,24 @@ def test_gemm_nan_scales_reach_their_rows_only(fmt, ws):
     assert R.same(product(LX, x, LW, w, FP32, ws), torch.from_numpy(want))
 
 
+@pytest.mark.parametrize("M,N", [(3, 140), (1030, 9472)])
+@pytest.mark.parametrize("fmt,xb,wb", [(0, [0, 1, 2], [252, 253, 254]), (0, [254, 253], [0, 1]), (1, list(range(8)), list(range(8))), (1, [0x7e, 1], [0x7e, 0x38])])
+def test_gemm_scales_at_the_ends_of_their_range(M, N, fmt, xb, wb, ws):
+    """Powers of two at both ends, one of which FP32 holds only as a subnormal number; subnormal E4M3 numbers, zeros, and the largest.  One
+    scale to a row, so that a sum is 64 products of codes, exact, times two scales."""
+    rng = np.random.default_rng(4)
+    K = 64
+    nb = K // R.BLOCK[fmt]
+    sides = []
+    for rows, choice in ((M, xb), (N, wb)):
+        code = rng.integers(0, 16, (rows, K)).astype(np.uint8)
+        byte = np.broadcast_to(rng.choice(choice, (rows, 1)), (rows, nb)).astype(np.uint8)
+        c, s = R.pack(code, byte, 0xFF)
+        sides.append((torch.from_numpy(c).cuda(), torch.from_numpy(s).cuda(), R.values(code, byte, fmt)))
+    Y = product(fq.fq_mx_get_layout(M, K, fmt), sides[0], fq.fq_mx_get_layout(N, K, fmt), sides[1], FP32, ws)
+    assert R.same(Y, torch.from_numpy((sides[0][2] @ sides[1][2].T).astype(np.float32)))
+
+
 def test_gemm_rows_of_y_with_a_stride(ws):
     rng = np.random.default_rng(2)
     for M, N, K in ((5, 130, 128), (140, 260, 512), (1030, 9401, 64)):
