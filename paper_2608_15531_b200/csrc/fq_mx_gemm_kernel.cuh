@@ -301,6 +301,7 @@ fq_mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
         cluster.sync();
         const uint32_t tn = first / p.tiles_m, tm = first - tn * p.tiles_m, m0 = tm * NT, rows = min((uint32_t)NT, p.M - m0);
         float alpha = 1.0f;
+        asm volatile("griddepcontrol.wait;" ::: "memory");     // (over long ago, but not every warp has asked)
         if (NV) alpha = (p.ts_x ? *(const volatile float*)p.ts_x : 1.0f) * (p.ts_w ? *(const volatile float*)p.ts_w : 1.0f);
         // A warp takes a token, a lane four of its features.  Eight loads in flight, of as many tokens as it takes (the
         // split is a power of two): number q is of the batch's token q / split, from rank q % split.
