@@ -262,21 +262,21 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// CTAs to an SM that the registers have to allow: 768 threads (80 registers; 4096 rows of 4096 with 512 threads 55 us, 768 50, 1024 67), one
-// CTA where each is alone on its SM.
+// CTAs to an SM that the registers have to allow: 768 threads (80 registers; 4096 rows of 4096 with 512 threads 55 us, 768 49, 1024 52 with
+// spills), one CTA where each is alone on its SM.
 constexpr int norm_ctas(int tpr, int v) { return v == 1 || tpr >= 768 ? 1 : 768 / (tpr < 128 ? 128 : tpr); }
 
 // TPR threads to a row, V vectors of eight values to a thread, which stay in registers from the sum to the last store: one
-// pass over the data.  A CTA goes through rows; the next row's values are on their way to shared memory meanwhile (each
-// thread copies and reads its own, so that no barrier is needed).  Rows of up to 512 values share a CTA (TPR = 32, a warp to a row).
+// pass over the data.  A CTA goes through rows; the next row's values are on their way to shared memory meanwhile, to the other of two places (each
+// thread copies and reads its own, so that no barrier is needed; values are read when they are wanted: with all of a row in registers 50 us).  Rows of up to 512 values share a CTA (TPR = 32, a warp to a row).
 // Sums and results run in binary64 (the product of a weight and a gate is exact in binary32).  In binary32 a value of H would
 // cross a border of its type in 1 of 10^4 cases, and a code of every tenth million be a step off.  What bounds it: 60 instructions
 // a value, half of them the sums over a row and what else a thread does once a row, on 59 % of the issue slots at three rows to an SM (80
 // registers); six conversions a value from and to binary64 keep their pipe 50 % busy.  4096 rows of 4096, with a norm behind the block, a gate
-// and everything put out 50 us (3.5 TB/s), without norm and gate 39; 2048 rows of 16384 99.
+// and everything put out 49 us (3.6 TB/s), without norm and gate 37; 2048 rows of 16384 103.
 template <class T, int TPR, int V, int FORMAT>                             // FORMAT: FQ_MXFP4, FQ_NVFP4, or 2 for none
 __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_ctas(TPR, V)) fq_norm_kernel(const NormParams p) {
-    extern __shared__ uint4 ahead[];                       // [V][3][threads]: the next row's X, block and gate
+    extern __shared__ uint4 ahead[];                       // [2][V][3][threads]: this and the next row's X, block and gate
     __shared__ double part[4][32];
     constexpr bool NV = FORMAT == (int)FQ_NVFP4;
     constexpr int RPC = TPR < 128 ? 128 / TPR : 1, THREADS = TPR * RPC;
@@ -286,21 +286,22 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_ctas(TPR, V)) fq_n
     const double inv_d = 1.0 / p.D;
     const uint4 zero = make_uint4(0, 0, 0, 0);
     auto column = [&](int j) { return (j * TPR + t) * 8; };
-    auto start = [&](uint32_t r) {                         // p.vec only: whole vectors
+    auto start = [&](uint32_t r, uint32_t half) {          // p.vec only: whole vectors
         if (r >= p.rows) return;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const uint32_t c = column(j), to = smem_u32(ahead + j * 3 * THREADS + threadIdx.x);
+            const uint32_t c = column(j), to = smem_u32(ahead + (half * V + j) * 3 * THREADS + threadIdx.x);
             if (c >= p.D) continue;
             copy16(to, (const T*)p.x + r * p.ld_x + c);
             if (p.block) copy16(to + THREADS * 16, (const T*)p.block + r * p.ld_block + c);
             if (gated) copy16(to + 2 * THREADS * 16, (const T*)p.gate + r * p.ld_gate + c);
         }
     };
+    uint32_t odd = 0;
     auto fetch = [&](const void* base, uint64_t at, int j, int slot) {
         const uint32_t c = column(j);
         if (!base || c >= p.D) return zero;
-        if (p.vec) return ahead[(j * 3 + slot) * THREADS + threadIdx.x];
+        if (p.vec) return ahead[((odd * V + j) * 3 + slot) * THREADS + threadIdx.x];
         return load_raw((const T*)base + at + c, (int)p.D - (int)c, false);
     };
     auto weight = [&](const void* base, int j, float (&v)[8]) {            // (from the L1 after the first row)
@@ -310,19 +311,12 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_ctas(TPR, V)) fq_n
         unpack8<T>(q, v);
     };
     grid_start();
-    if (p.vec) start(row);
+    if (p.vec) start(row, 0);
     TensorScale ts;
     if constexpr (NV) ts.read(p.ts);
-    for (uint32_t odd = 0; row < p.rows; row += stride, odd ^= 1) {        // (whole warps; all warps of a CTA of one row)
+    for (; row < p.rows; row += stride, odd ^= 1) {        // (whole warps; all warps of a CTA of one row)
         if (p.vec) asm volatile("cp.async.wait_all;" ::: "memory");
-        uint4 x[V], o[V], g[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            x[j] = fetch(p.x, row * p.ld_x, j, 0);
-            o[j] = fetch(p.block, row * p.ld_block, j, 1);
-            g[j] = fetch(p.gate, row * p.ld_gate, j, 2);
-        }
-        if (p.vec) start(row + stride);
+        if (p.vec) start(row + stride, odd ^ 1);
         double r[V][8];
         double c1 = p.alpha;
         if (post) {
@@ -330,7 +324,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_ctas(TPR, V)) fq_n
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 float v[8];
-                unpack8<T>(o[j], v);
+                unpack8<T>(fetch(p.block, row * p.ld_block, j, 1), v);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     r[j][i] = (double)v[i];
@@ -345,12 +339,12 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_ctas(TPR, V)) fq_n
             float v[8], b[8];
             if (p.block) {
                 if (!post) {
-                    unpack8<T>(o[j], v);
+                    unpack8<T>(fetch(p.block, row * p.ld_block, j, 1), v);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) r[j][i] = (double)v[i];
                 }
                 if (post || gated) {
-                    if (gated) unpack8<T>(g[j], b);
+                    if (gated) unpack8<T>(fetch(p.gate, row * p.ld_gate, j, 2), b);
                     if (post) {
                         weight(p.block_weight, j, v);
 #pragma unroll
@@ -360,7 +354,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_ctas(TPR, V)) fq_n
                     for (int i = 0; i < 8; ++i) r[j][i] *= (double)b[i];
                 }
             }
-            unpack8<T>(x[j], v);
+            unpack8<T>(fetch(p.x, row * p.ld_x, j, 0), v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 r[j][i] = p.block ? fma(r[j][i], c1, (double)v[i]) : (double)v[i];
@@ -512,7 +506,7 @@ static fq_status_t launch_mx(MxFn fn, MxParams& p, uint32_t G, void* stream) {
 
 typedef void (*NormFn)(const NormParams);
 // `tpr`: threads to a row, `v`: vectors of eight to a thread.  Two, which halves what a thread spends on the sums over the row (4096 rows
-// of 4096 50 us, with one 61); but one where every row has an SM to itself and only latency counts.
+// of 4096 49 us, with one 61); but one where every row has an SM to itself and only latency counts.
 template <class T, int FORMAT>
 static NormFn pick_norm(uint32_t D, bool few, uint32_t& tpr, uint32_t& v) {
     const uint32_t vectors = (D + 7) / 8;
@@ -791,7 +785,7 @@ fq_status_t fq_norm_block(const fq_norm_args_t* a, void* cuda_stream) {
     uint32_t tpr = 0, v = 0;
     const bool few = a->rows <= (uint32_t)sms;
     const NormFn fn = a->type == FQ_TYPE_BF16 ? pick_norm<__nv_bfloat16>(format, a->D, few, tpr, v) : pick_norm<__half>(format, a->D, few, tpr, v);
-    const uint32_t threads = std::max<uint32_t>(tpr, 128), per = threads / tpr, smem = 48 * v * threads;
+    const uint32_t threads = std::max<uint32_t>(tpr, 128), per = threads / tpr, smem = 96 * v * threads;
     const cudaError_t e = ensure_smem_attr((const void*)fn, (int)smem);
     if (e != cudaSuccess) return fail(FQ_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
     const uint32_t grid = std::min<uint32_t>((a->rows + per - 1) / per, (uint32_t)(sms * ctas_per_sm((const void*)fn, (int)threads, smem)));
