@@ -394,8 +394,8 @@ fq_status_t fq_mx_sizes(const fq_mx_layout_t* L, size_t* code_bytes, size_t* sca
 fq_status_t fq_mx_quantize(const fq_mx_layout_t* L, const void* X, uint32_t type, uint64_t ldx, const float* tensor_scale,
                            void* codes, void* scales, void* cuda_stream);
 
-/* The gated product of a decoder's MLP, quantised: h = gate / (1 + exp(-gate)) * up, rounded once to `type` (FQ_TYPE_BF16 or
- * FQ_TYPE_FP16), then as fq_mx_quantize.  gate, up: device, rows x K, row strides ld_gate and ld_up (the halves of one
+/* The gated product of a decoder's MLP, quantised: h = gate / (1 + exp(-gate)) * up, the exact value rounded to `type` (FQ_TYPE_BF16 or
+ * FQ_TYPE_FP16) by way of binary32, then as fq_mx_quantize.  gate, up: device, rows x K, row strides ld_gate and ld_up (the halves of one
  * rows x 2K array, for instance). */
 fq_status_t fq_mx_quantize_swiglu(const fq_mx_layout_t* L, const void* gate, uint64_t ld_gate, const void* up, uint64_t ld_up,
                                   uint32_t type, const float* tensor_scale, void* codes, void* scales, void* cuda_stream);
@@ -412,8 +412,8 @@ fq_status_t fq_mx_dequantize(const fq_mx_layout_t* L, const void* codes, const v
  *     y = block * rsqrt(mean(block^2) + eps) * block_weight  (with it)
  *     r = X + residual_scale * gate * y                      (r = X without block; gate 1 without gate)
  *     h = r * rsqrt(mean(r^2) + eps) * weight                (weight 1 without weight)
- * r and h are each rounded once (h is computed from the unrounded r), codes and scales are those that fq_mx_quantize makes
- * of the rounded h.  Sums run in binary64, and a result too near a rounding border for binary32 is settled in binary64.
+ * All of it in binary64 (eps and residual_scale are the given binary32 numbers); r and h are each rounded at the end, by way of binary32, h
+ * computed from the unrounded r; codes and scales are those that fq_mx_quantize makes of the rounded h.
  * Any of R, H and (codes, scales) may be null, not all.  All of `type`, FQ_TYPE_BF16 or FQ_TYPE_FP16; vectors of D on any
  * boundary; D from 1 to FQ_NORM_MAX_D; with codes, layout.rows = rows and layout.K = D.
  * R or H may be X or block themselves (same address and row stride): the sum in place.

@@ -480,8 +480,10 @@ static MxParams mx_params(const fq_mx_layout_t* L, const float* ts) {
     return p;
 }
 typedef void (*MxFn)(const MxParams);
-// Rows that a warp takes: four, unless that leaves SMs without a warp.
-static bool one_row_tasks(const MxParams& p) { return (uint64_t)p.rows * p.chunks <= 32ull * p.sms; }
+// Rows that a warp takes: four for large matrices (28672 x 4096 of BF16, MXFP4, us, one / four 51.3 / 45.4, NVFP4 93 / 76, read back 48.8 /
+// 46.4; 8192 x 4096 16.0 / 15.9, 28.3 / 25.9, 13.1 / 11.8), one for others, whose time is that of a warp (4096 x 4096 8.7 / 9.7, 15.3 / 15.9, 6.7 / 7.0;
+// 1024 x 4096 2.7 / 3.8, 4.8 / 7.7, 2.6 / 4.0).
+static bool one_row_tasks(const MxParams& p) { return (uint64_t)p.rows * p.chunks <= 256ull * p.sms; }
 template <class T, bool GATED>
 static MxFn pick_quantize(bool nv, bool one) {
     constexpr int G = GATED ? 1 : 4;
@@ -497,8 +499,8 @@ static MxFn pick_dequantize(bool nv, bool one) {
 static fq_status_t launch_mx(MxFn fn, MxParams& p, uint32_t G, void* stream) {
     // lines of tasks: the first 32 rows of each 32 G (rows 32 further on go with them)
     p.tasks = ((uint64_t)(p.rows / (32 * G)) * 32 + std::min<uint32_t>(p.rows % (32 * G), 32)) * p.chunks;
-    // (few warps: CTAs of two, so that they are spread over the SMs)
-    const uint32_t threads = p.tasks <= 32ull * p.sms ? 64 : kMxThreads;
+    // few warps in CTAs of two, so that they are spread over the SMs (MXFP4, us, two / eight warps: 256 x 4096 1.6 / 1.8, 512 x 4096 2.6 / 2.2)
+    const uint32_t threads = p.tasks <= 16ull * p.sms ? 64 : kMxThreads;
     const uint64_t warps = threads / 32, ctas = (p.tasks + warps - 1) / warps;
     if (ctas > 0x7fffffffull) return fail(FQ_ERR_UNSUPPORTED_SHAPE, "matrix too large for one launch");
     return launch(fn, dim3((uint32_t)ctas), threads, 0, 1, stream, p);
@@ -634,11 +636,13 @@ static fq_status_t launch_mx_pair(const fq_mx_layout_t* LX, const void* xc, cons
     if (e != cudaSuccess) return fail(FQ_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
     return launch(fn, dim3(2 * std::min(p.tiles, sms / 2)), 32 * kPairWarps, smem, 1, stream, mw, mx, mws, mxs, p);
 }
-// Tokens of a tile of the pair kernel: 256, unless tiles of 128 leave the busiest pair less to do.
+// Tokens of a tile of the pair kernel, 128 or 256: what leaves the busiest pair the fewest bytes to copy, which is what its time goes by (a step's
+// codes and scales of 256 features, and of the tokens that a tile has).  us, 128 / 256: 129 x 4096 x 19200 12.6 / 10.7, 200 x 4096 x 28672 18.0 /
+// 13.8, 2048 x 4096 x 4096 16.5 / 15.0, 640 x 4096 x 28672 44.3 / 38.9; 1024 x 4096 x 6144, the other way, 13.7 / 14.4.
 static uint32_t pair_tokens(uint32_t M, uint32_t N, uint32_t sms) {
     auto work = [&](uint32_t t) {
-        const uint64_t tiles = (uint64_t)((M + t - 1) / t) * ((N + 255) / 256), pairs = sms / 2;
-        return (tiles + pairs - 1) / pairs * t;
+        const uint64_t tiles_m = (M + t - 1) / t, tiles = tiles_m * ((N + 255) / 256), pairs = sms / 2;
+        return (tiles + pairs - 1) / pairs * (19 + M / tiles_m / 16);
     };
     return work(128) < work(256) ? 128 : 256;
 }

@@ -246,7 +246,7 @@ def ws():
 @pytest.mark.parametrize("fmt", [0, 1])
 @pytest.mark.parametrize("M,N,K", [(1, 1, 32), (1, 128, 64), (1, 129, 96), (2, 100, 160), (16, 256, 256), (17, 130, 288), (32, 127, 512), (33, 384, 544),
                                    (64, 200, 1024), (65, 129, 992), (100, 64, 2048), (128, 300, 320), (129, 257, 736), (300, 333, 1056), (520, 700, 416),
-                                   (1, 4096, 1024), (3, 513, 2048), (777, 130, 96), (1, 20000, 128), (1000, 2000, 64), (1011, 9400, 160), (1040, 9472, 544), (1160, 9300, 96), (129, 19200, 96), (150, 19300, 320)])
+                                   (1, 4096, 1024), (3, 513, 2048), (777, 130, 96), (1, 20000, 128), (1000, 2000, 64), (1011, 9400, 160), (1040, 9472, 544), (1160, 9300, 96), (129, 19200, 96), (150, 19300, 320), (260, 9500, 288), (384, 9500, 64)])
 def test_gemm_exact_sums(M, N, K, fmt, ws):
     """Products are multiples of 2^-4 of magnitude up to 144, and K of them below 2^18: each sum has at most 24 bits,
     in whatever order, so that the result is the exact one rounded once."""
