@@ -47,7 +47,7 @@ struct MxGemm {
     static constexpr uint32_t STAGE = W_BYTES + X_BYTES + 2 * S_BYTES;
     static constexpr uint32_t OFF_X = W_BYTES, OFF_WS = OFF_X + X_BYTES, OFF_XS = OFF_WS + S_BYTES;
     // tensor memory: accumulators, then the scales of a stage
-    static constexpr uint32_t ACCS = 1, D_COLS = ACCS * NT, COL_WS = D_COLS, COL_XS = COL_WS + ATOMS * 4, USED = COL_XS + ATOMS * 4;
+    static constexpr uint32_t COL_WS = NT, COL_XS = COL_WS + ATOMS * 4, USED = COL_XS + ATOMS * 4;
     static constexpr uint32_t COLS = USED <= 64 ? 64 : (USED <= 128 ? 128 : (USED <= 256 ? 256 : 512));
     static_assert(STAGE % 1024 == 0 && COLS <= 256, "stage, tensor memory of two CTAs");
     // Two CTAs to an SM: the one drains while the other multiplies, and the next launch's start beside this one's.
@@ -164,19 +164,18 @@ fq_mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                   const __grid_constant__ CUtensorMap map_xs, const MxGemmParams p) {
     using G = MxGemm<NT, NV>;
     extern __shared__ uint8_t mx_smem[];
-    __shared__ uint64_t bars[2 * kMxStages + 2 * G::ACCS + 1];
+    __shared__ uint64_t bars[2 * kMxStages + 3];
     __shared__ uint32_t tmem_slot;
     __shared__ uint32_t abort_word;
     namespace cg = cooperative_groups;
     // (the shuffle tells the compiler that a warp's lanes agree: the tensor warp's operands then stay in uniform registers)
     const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x & 31, S = p.stages;
     const uint32_t smem = (smem_u32(mx_smem) + 1023) & ~1023u;
-    const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * kMxStages, bar_acc = bar_empty + 8 * kMxStages, bar_free = bar_acc + 8 * G::ACCS, bar_final = bar_free + 8 * G::ACCS;
+    const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * kMxStages, bar_acc = bar_empty + 8 * kMxStages, bar_free = bar_acc + 8, bar_final = bar_free + 8;
     volatile uint32_t* abort_flag = &abort_word;
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < S; ++s) mbar_init(bar_full + 8 * s, 1), mbar_init(bar_empty + 8 * s, 1);
-        for (uint32_t i = 0; i < G::ACCS; ++i) mbar_init(bar_acc + 8 * i, 1), mbar_init(bar_free + 8 * i, G::DRAIN);
-        mbar_init(bar_final, 1);
+        mbar_init(bar_acc, 1), mbar_init(bar_free, G::DRAIN), mbar_init(bar_final, 1);
         abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -229,11 +228,11 @@ fq_mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
         w.cw = tmem + G::COL_WS, w.cx = tmem + G::COL_XS, w.tiles_x = 1;
         w.s_hi = (uint32_t)(desc_plain(0, 128) >> 32), w.hi = (uint32_t)(desc_sw128(0) >> 32);
         const uint32_t codes0 = (uint32_t)desc_sw128(smem), scales0 = (uint32_t)desc_plain(smem, 128);
-        uint32_t s = 0, ph = 0, acc = 0, aph = 0;
+        w.d = tmem;
+        uint32_t s = 0, ph = 0, aph = 0;
         for (uint32_t tile = first; tile < p.tiles; tile += stride) {
-            if (!warp_wait(bar_free + 8 * acc, aph ^ 1, abort_flag, p.status)) break;
+            if (!warp_wait(bar_free, aph ^ 1, abort_flag, p.status)) break;
             tc_fence_after();
-            w.d = tmem + acc * NT;
             bool ok = true;
             for (uint32_t k = k0; k < k1; ++k) {
                 if (!(ok = warp_wait(bar_full + 8 * s, ph, abort_flag, p.status))) break;
@@ -244,11 +243,11 @@ fq_mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                 w.mmas = (min(p.K - k * kMxStageK, kMxStageK) + 63) / 64;  // (beyond K the scales are not there)
                 stage_one<NV>(w);
                 commit_elected(bar_empty + 8 * s);
-                if (k + 1 == k1) commit_elected(bar_acc + 8 * acc);
+                if (k + 1 == k1) commit_elected(bar_acc);
                 if (++s == S) s = 0, ph ^= 1;
             }
             if (!ok) break;
-            if (++acc == G::ACCS) acc = 0, aph ^= 1;
+            aph ^= 1;
         }
         // No MMA is in flight when the tensor memory is given back and the CTA leaves, whoever gave up.
         commit_elected(bar_final);
@@ -264,17 +263,17 @@ fq_mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
             alpha = a * b;
         }
         const uint32_t quarter = warp & 3, half = (warp - 4) / 4, f = quarter * 32 + lane;             // (two warps take 32 tokens in turn)
-        uint32_t acc = 0, aph = 0;
+        uint32_t aph = 0;
         constexpr int C = NT < 32 ? NT : 32;
-        for (uint32_t tile = first; tile < p.tiles; tile += stride) {
-            if (!warp_wait(bar_acc + 8 * acc, aph, abort_flag, p.status)) break;
+        for (uint32_t tile = first; tile < p.tiles; tile += stride, aph ^= 1) {
+            if (!warp_wait(bar_acc, aph, abort_flag, p.status)) break;
             tc_fence_after();
             const uint32_t tn = tile / p.tiles_m, tm = tile - tn * p.tiles_m, n = tn * 128 + f, m0 = tm * NT;
             const uint32_t rows = min((uint32_t)NT, p.M - m0);
             T* y = (T*)p.Y + (uint64_t)m0 * p.ldy + n;
             for (uint32_t c = C * half; c < rows; c += C * (G::DRAIN / 4)) {
                 float v[C];
-                tmem_ld<C>(tmem + (quarter << 21) + acc * NT + c, v);
+                tmem_ld<C>(tmem + (quarter << 21) + c, v);
                 tmem_wait_ld();
                 if (p.split > 1) {
                     float* part = reinterpret_cast<float*>(mx_smem + (smem - smem_u32(mx_smem))) + c * 128 + f;
@@ -285,8 +284,7 @@ fq_mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                 }
             }
             tc_fence_before();
-            if (lane == 0) mbar_arrive(bar_free + 8 * acc);
-            if (++acc == G::ACCS) acc = 0, aph ^= 1;
+            if (lane == 0) mbar_arrive(bar_free);
         }
     }
 
@@ -349,8 +347,8 @@ fq_mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
 // rounded up to 32.
 // What bounds it: of the 12500 clocks of a tile of 4096 k the MMAs need 8200 (tensor pipe 68 % busy); 1700 pass between a tile's last
 // MMA and the next one's first (commit, tensor memory to registers, arrival from the other CTA), the rest waits for copies: six
-// stages of 35 KB are all the shared memory, and the L2 delivers 13 TB/s.  4096 x 4096 x 28672 197 us on one set of operands (4.9 PFLOP/s), 219 on
-// three in turn; 1024 x 4096 x 18944 29 (5.4 PFLOP/s).  Copies of the next tile's weights to the L2 ahead of time changed nothing.
+// stages of 35 KB are all the shared memory, and the L2 delivers 13 TB/s.  4096 x 4096 x 28672 164 us for the first milliseconds (5.9 PFLOP/s),
+// 197 to 220 once the power cap has lowered the clock to 1.6 GHz; 1024 x 4096 x 18944 29 (5.4 PFLOP/s).  Copies of the next tile's weights to the L2 ahead of time changed nothing.
 constexpr uint32_t kPairWarps = 12;        // copies, MMAs, allocation, one idle; eight drain warps: two for each 32 features
 
 struct MxPairParams {

@@ -269,7 +269,7 @@ constexpr int norm_ctas(int tpr, int v) { return v == 1 || tpr >= 768 ? 1 : 768 
 // TPR threads to a row, V vectors of eight values to a thread, which stay in registers from the sum to the last store: one
 // pass over the data.  A CTA goes through rows; the next row's values are on their way to shared memory meanwhile, to the other of two places (each
 // thread copies and reads its own, so that no barrier is needed; values are read when they are wanted: with all of a row in registers 50 us).  Rows of up to 512 values share a CTA (TPR = 32, a warp to a row).
-// Sums and results run in binary64 (the product of a weight and a gate is exact in binary32).  In binary32 a value of H would
+// Sums and results run in binary64 (the product of a weight and a gate is exact in binary32, within its range).  In binary32 a value of H would
 // cross a border of its type in 1 of 10^4 cases, and a code of every tenth million be a step off.  What bounds it: 60 instructions
 // a value, half of them the sums over a row and what else a thread does once a row, on 59 % of the issue slots at three rows to an SM (80
 // registers); six conversions a value from and to binary64 keep their pipe 50 % busy.  4096 rows of 4096, with a norm behind the block, a gate
