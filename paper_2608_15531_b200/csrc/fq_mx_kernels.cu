@@ -79,12 +79,12 @@ __device__ __forceinline__ float gated(float g, float u) {
 __device__ __noinline__ float gated_exact(float g, float u) { return (float)((double)g / (1.0 + exp(-(double)g)) * (double)u); }
 
 // A lane's 16 gated products, rounded to T and quantised.  The exact product lies between the computed one a little less and a little
-// more; where both round alike that is the result.  Where some do not (1 in 3000 values of BF16, 1 in 400 of FP16), but
+// more; where both round alike that is the result.  Where some do not (1 in 4000 values of BF16, 1 in 500 of FP16), but
 // give the same codes and scales, no matter (h itself is not put out); else (one in some thousand warps) the warp takes what
 // is in question in binary64.  `again`: loads gate and up once more.
 template <class T, bool NV, class F>
 __device__ __forceinline__ void quantize_gated16(const Words8& gate, const Words8& up, F&& again, const TensorScale& ts, uint2& codes, uint32_t& scale) {
-    constexpr float E = 0x1p-20f;
+    constexpr float E = 0x1.8p-21f;                        // 6 * 2^-23: the bound, and half a unit for the step's own rounding
     Words8 hi;                                             // the larger magnitude; the smaller one is hi, or the number below it where
     uint32_t below = 0;                                    // below has a bit: i and 16 + i for the two of word i
 #pragma unroll
