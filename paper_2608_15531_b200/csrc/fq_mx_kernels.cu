@@ -32,8 +32,8 @@ __device__ __forceinline__ void grid_start() {
 // more warps, and gated products, which are bound by instructions, keep to 64 registers.  16 values are a block of FQ_NVFP4, whose scale (a quotient and its rounding) is then
 // computed by one lane.
 // Measured (28672 x 4096 of BF16): MXFP4 45.6 us (6.5 TB/s, the rate of a copy), reading back 46.4; NVFP4 56.3 (5.3 TB/s: 11.8 instructions a
-// value, each rounded twice to see whether the quotient is near a border, 65 % of the issue slots).  Gated products, 4096 x 14336: 69 us (MXFP4, BF16;
-// 30 instructions a value, 72 % of the issue slots, and two of them on the quarter-rate pipe) and 89.5 (NVFP4, FP16; 42).
+// value, each rounded twice to see whether the quotient is near a border, 65 % of the issue slots).  Gated products, 4096 x 14336: 64.4 us (MXFP4, BF16;
+// under 30 instructions a value, 72 % of the issue slots, and two of them on the quarter-rate pipe) and 87 (NVFP4, FP16; about 40).
 struct MxParams {
     const void* a;               // X, or the gate
     const void* b;               // up
@@ -64,12 +64,21 @@ struct MxTask {
 };
 constexpr int kMxThreads = 256;
 
-// gate / (1 + exp(-gate)) * up in binary32.  exp(-g) is 2^t (1 + c), where t is -g log2(e) as rounded and c = -g - t ln(2), what the
-// rounding left (below 2^-17).  Off by at most 2^-22 (ex2) + 2^-23 (rcp) and four roundings, 5 * 2^-23 of the result, as
-// long as the gate is not below -80, where 1 + exp(-g) may leave binary32.
+// gate / (1 + exp(-gate)) * up in binary32, off by at most 5.5 * 2^-23 of the result as long as the gate is not below -60 (far below that 1 +
+// exp(-g) leaves binary32): 2^-22 (ex2), 2^-23 (rcp), four roundings and, BF16, half a unit.  exp(-g) is 2^t (1 + c) with
+//   FP16   t = -g log2(e) as rounded, c = -g - t ln(2), what the rounding left (below 2^-17)
+//   BF16   t = -g H, exact: H is log2(e) cut to 16 bits, and c = -g (log2(e) - H) ln(2), whose square (below 2^-23.3) is left out
+template <class T>
 __device__ __forceinline__ float gated(float g, float u) {
-    constexpr float L = 1.44269504f, N = 0.693147181f, N2 = -1.90465421e-9f;      // log2(e); ln(2) and what binary32 leaves of it
-    const float t = -L * g, c = fmaf(-N2, t, fmaf(-N, t, -g));
+    float t, c;
+    if constexpr (IsBf16<T>::value) {
+        t = -1.44268798828125f * g;
+        c = -4.88849543e-6f * g;
+    } else {
+        constexpr float L = 1.44269504f, N = 0.693147181f, N2 = -1.90465421e-9f;  // log2(e); ln(2) and what binary32 leaves of it
+        t = -L * g;
+        c = fmaf(-N2, t, fmaf(-N, t, -g));
+    }
     float e, s;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
     e = fmaf(e, c, e) + 1.0f;
@@ -84,19 +93,19 @@ __device__ __noinline__ float gated_exact(float g, float u) { return (float)((do
 // is in question in binary64.  `again`: loads gate and up once more.
 template <class T, bool NV, class F>
 __device__ __forceinline__ void quantize_gated16(const Words8& gate, const Words8& up, F&& again, const TensorScale& ts, uint2& codes, uint32_t& scale) {
-    constexpr float E = 0x1.8p-21f;                        // 6 * 2^-23: the bound, and half a unit for the step's own rounding
+    constexpr float E = 0x1.8p-21f;                        // 6 * 2^-23: the bound, and half a unit for the step's rounding
     Words8 hi;                                             // the larger magnitude; the smaller one is hi, or the number below it where
     uint32_t below = 0;                                    // below has a bit: i and 16 + i for the two of word i
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float2 g = unpack2(gate.w[i], T()), u = unpack2(up.w[i], T());
-        const float a = gated(g.x, u.x), b = gated(g.y, u.y);
+        const float a = gated<T>(g.x, u.x), b = gated<T>(g.y, u.y);
         hi.w[i] = pack2(a * (1.0f + E), b * (1.0f + E), T());
         below += (hi.w[i] - pack2(a * (1.0f - E), b * (1.0f - E), T())) << i;
     }
-    // the gate's bits as an unsigned number are above those of -80 where it is below -80 (or a NaN with a sign)
+    // the gate's bits as an unsigned number are above those of -60 where it is below -60 (or a NaN with a sign)
     constexpr bool BF = IsBf16<T>::value;
-    constexpr uint32_t deep = BF ? 0xc2a0u : 0xd500u;
+    constexpr uint32_t deep = BF ? 0xc270u : 0xd380u;
     const uint4 g0 = gate.half(0), g1 = gate.half(1);
     const uint32_t gm = max_u16x2(max_u16x2(max_u16x2(g0.x, g0.y), max_u16x2(g0.z, g0.w)), max_u16x2(max_u16x2(g1.x, g1.y), max_u16x2(g1.z, g1.w)));
     // products so small that binary32 may have lost bits on the way: only where a whole block is
