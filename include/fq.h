@@ -367,7 +367,9 @@ fq_status_t fq_fused_host_io_async(const fq_layout_t* L, const void* X_host, uin
  * All calls take any number of rows from 1, enqueue on the stream and return.  Unlike the weights of the fused INT4 call,
  * every array may be written by a kernel that is still running in the stream when the call is made: each kernel
  * here waits for the grid before it before it reads or writes anything.
- * Outputs must not overlap inputs or each other (FQ_ERR_INVALID_ARG), except where it is said.
+ * Outputs must not overlap inputs or each other (FQ_ERR_INVALID_ARG), except where it is said.  What lies between the rows of an array is
+ * not part of it: column slices of one array may be outputs and inputs of a call.  Two arrays whose rows lie apart with different
+ * strides are refused wherever their address ranges overlap.
  */
 #define FQ_MXFP4 0u
 #define FQ_NVFP4 1u

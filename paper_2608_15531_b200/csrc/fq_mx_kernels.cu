@@ -15,6 +15,7 @@
 #include "fq_launch.h"
 #include "fq_mx.cuh"
 #include "fq_mx_gemm_kernel.cuh"
+#include "fq_overlap.h"
 #include "fq_ptx.cuh"
 #include "fq_shares.h"
 
@@ -454,27 +455,6 @@ static bool mx_layout_ok(const fq_mx_layout_t* L) {
     return L && L->abi == FQ_ABI_VERSION && L->format <= FQ_NVFP4 && L->rows && L->rows <= FQ_MX_MAX_ROWS && L->K && L->K % 32 == 0 && L->K <= FQ_MX_MAX_K;
 }
 
-// A piece of memory that a call reads or writes.
-struct Piece {
-    const void* p;
-    size_t bytes;
-    bool overlaps(const Piece& o) const {
-        const uintptr_t a = (uintptr_t)p, b = (uintptr_t)o.p;
-        return p && o.p && bytes && o.bytes && a < b + o.bytes && b < a + bytes;
-    }
-};
-// rows x cols values of `size` bytes with a row stride of ld values
-static Piece matrix(const void* p, uint64_t rows, uint64_t cols, uint64_t ld, size_t size) { return Piece{p, (size_t)(((rows - 1) * ld + cols) * size)}; }
-// No output on another output or on an input.
-static bool disjoint(const Piece* out, int nout, const Piece* in, int nin) {
-    for (int i = 0; i < nout; ++i) {
-        for (int j = i + 1; j < nout; ++j)
-            if (out[i].overlaps(out[j])) return false;
-        for (int j = 0; j < nin; ++j)
-            if (out[i].overlaps(in[j])) return false;
-    }
-    return true;
-}
 static fq_status_t check_stride(const char* what, const void* p, uint64_t rows, uint64_t cols, uint64_t ld, size_t size) {
     if (!aligned(p, size)) return fail(FQ_ERR_INVALID_ARG, "%s is misaligned", what);
     if ((rows > 1 && ld < cols) || ld > (1ull << 40) || (rows - 1) > (1ull << 56) / (ld + 1)) return fail(FQ_ERR_INVALID_ARG, "%s: row stride %llu for %llu columns", what, (unsigned long long)ld, (unsigned long long)cols);

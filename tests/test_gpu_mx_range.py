@@ -58,3 +58,34 @@ def test_norm_block_gate_times_weight_at_the_ends_of_fp16(D):
         fq.fq_norm_block(torch.zeros(3, D, dtype=FP16, device="cuda"), 1e-6, block=block.cuda(), block_weight=weight.cuda(), gate=gate.cuda(), residual_scale=alpha,
                          R=Rd, H=Hd)
         assert R.same(Rd, R.round_to(r, FP16)) and R.same(Hd, R.round_to(h, FP16))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("rows,D,pad", [(2, 32, 0), (700, 96, 0), (37, 160, 3), (1200, 4096, 0)])
+def test_norm_block_on_column_slices_of_one_array(rows, D, pad, dtype):
+    """Inputs, R and H lie beside each other in the rows of one array; what is between them stays as it is."""
+    rng = torch.Generator().manual_seed(rows + D)
+    wide = torch.randn(rows, 5 * D + pad, generator=rng).to(dtype)
+    x, block, gate = (wide[:, i * D:(i + 1) * D] for i in (0, 2, 4))
+    r, h = R.norm_block(R.f64(x), 1e-5, R.f64(block), None, R.f64(gate), 0.5)
+    want = wide.clone()
+    want[:, D:2 * D], want[:, 3 * D:4 * D] = R.round_to(r, dtype), R.round_to(h, dtype)
+    d = wide.cuda()
+    x, Rd, block, Hd, gate = (d[:, i * D:(i + 1) * D] for i in range(5))
+    fq.fq_norm_block(x, 1e-5, block=block, gate=gate, residual_scale=0.5, R=Rd, H=Hd)
+    assert R.same(d, want)
+    with pytest.raises(fq.FqError, match="overlaps"):
+        fq.fq_norm_block(x, 1e-5, block=block, R=Rd, H=d[:, 3 * D - 1:4 * D - 1])
+
+
+def test_read_back_beside_another_matrix():
+    """Two matrices of values in one array, read back in turn, each from codes that the call before made of the other."""
+    rows, K = 300, 96
+    L = fq.fq_mx_get_layout(rows, K, 0)
+    wide = torch.randn(rows, 2 * K, generator=torch.Generator().manual_seed(2)).to(BF16)
+    want = R.round_to(R.values(*R.quantize(R.f64(wide[:, :K]), 0), 0), BF16)
+    d = wide.cuda()
+    codes, scales = (torch.zeros(n, dtype=torch.uint8, device="cuda") for n in fq.fq_mx_sizes(L))
+    fq.fq_mx_quantize(L, d[:, :K], codes, scales)
+    fq.fq_mx_dequantize(L, codes, scales, d[:, K:])
+    assert R.same(d[:, K:], want) and torch.equal(d[:, :K].cpu(), wide[:, :K])
