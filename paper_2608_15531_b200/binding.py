@@ -271,7 +271,11 @@ def fq_fused_host_io_async(L: Layout, X_host, M: int, x_dev, wq, scale, zero, ti
 
 
 def fq_check_status(workspace, stream=None) -> None:
-    _check(lib().fq_check_status(_dp(workspace), _stream(stream)))
+    """Waits for the stream (None: the current stream of the workspace's device) and raises what a call on this workspace reported."""
+    import torch
+    p = _dp(workspace)
+    with torch.cuda.device(workspace.device):
+        _check(lib().fq_check_status(p, _stream(stream)))
 
 
 def fq_last_error() -> str:
