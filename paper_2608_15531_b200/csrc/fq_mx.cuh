@@ -101,16 +101,16 @@ template <class T>
 __device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
     return make_uint4(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()), pack2(v[4], v[5], T()), pack2(v[6], v[7], T()));
 }
-// p[0..7], of which only the first `n` exist (the others are 0); `vec`: all do, on a 16-byte boundary.
+// p[0..7] on any boundary, of which only the first `n` exist (the others are 0).
 template <class T>
-__device__ __forceinline__ uint4 load_raw(const T* p, int n, bool vec) {
-    if (vec) return ld16(p);
+__device__ __forceinline__ uint4 load_raw(const T* p, int n) {
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (i < n) w[i / 2] |= (uint32_t)reinterpret_cast<const volatile uint16_t*>(p)[i] << (16 * (i & 1));
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
+// The same way back; `vec`: all exist, on a 16-byte boundary.
 template <class T>
 __device__ __forceinline__ void store_raw(T* p, int n, bool vec, const uint4& q) {
     if (vec) {

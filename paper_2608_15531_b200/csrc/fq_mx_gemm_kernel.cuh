@@ -53,7 +53,7 @@ struct MxGemm {
     // Two CTAs to an SM: the one drains while the other multiplies, and the next launch's start beside this one's.
     static constexpr uint32_t STAGES = (113 * 1024 - 2048) / STAGE, STAGES_ALONE = (kSmemBudget - 2048) / STAGE;
     static constexpr uint32_t DRAIN = NT >= 64 ? 8 : 4, THREADS = 128 + 32 * DRAIN;        // drain warps: one or two for each 32 features
-    static_assert(STAGES >= 3 && STAGES * STAGE >= NT * 128 * 4, "stages, exchange of a split tile");
+    static_assert(STAGES >= 3 && STAGES_ALONE <= kMxStages && STAGES * STAGE >= NT * 128 * 4, "stages, exchange of a split tile");
 };
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t x, uint32_t y, uint32_t z, uint32_t bar) {
@@ -368,6 +368,7 @@ struct MxPair {
     static constexpr uint32_t COL_WS = 256, COL_XS = COL_WS + ATOMS * 4, USED = COL_XS + ATOMS * 8;
     static_assert(USED <= 512 && STAGE % 1024 == 0, "tensor memory, swizzle");
     static constexpr uint32_t STAGES = (kSmemBudget - 2048) / STAGE;
+    static_assert(STAGES <= 8, "barriers");
 };
 // Tokens that a tile multiplies; each CTA holds half of them.
 __device__ __forceinline__ uint32_t pair_tile_tokens(const MxPairParams& p, uint32_t m0) { return min(p.tokens, (p.M - m0 + 31) / 32 * 32); }

@@ -178,8 +178,6 @@ __global__ void __launch_bounds__(kMxThreads, sizeof(T) == 2 ? (GATED || NV ? 4 
         uint8_t* to = p.scales + scale_word(task.row0, p.atoms, atom);
         if (G == 4 && task.row0 + 96 < p.rows) {
             *reinterpret_cast<uint4*>(to) = make_uint4(words[0], words[1 % G], words[2 % G], words[3 % G]);
-        } else if (G == 2 && task.row0 + 32 < p.rows) {
-            *reinterpret_cast<uint2*>(to) = make_uint2(words[0], words[1 % G]);
         } else {
 #pragma unroll
             for (int g = 0; g < G; ++g)
@@ -314,12 +312,12 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_ctas(TPR, V)) fq_n
         const uint32_t c = column(j);
         if (!base || c >= p.D) return zero;
         if (p.vec) return ahead[((odd * V + j) * 3 + slot) * THREADS + threadIdx.x];
-        return load_raw((const T*)base + at + c, (int)p.D - (int)c, false);
+        return load_raw((const T*)base + at + c, (int)p.D - (int)c);
     };
     auto weight = [&](const void* base, int j, float (&v)[8]) {            // (from the L1 after the first row)
         const uint32_t c = column(j);
         uint4 q = zero;
-        if (c < p.D) q = p.vec ? *reinterpret_cast<const uint4*>((const T*)base + c) : load_raw((const T*)base + c, (int)p.D - (int)c, false);
+        if (c < p.D) q = p.vec ? *reinterpret_cast<const uint4*>((const T*)base + c) : load_raw((const T*)base + c, (int)p.D - (int)c);
         unpack8<T>(q, v);
     };
     grid_start();
@@ -605,10 +603,10 @@ static fq_status_t launch_mx_gemm(const fq_mx_layout_t* LX, const void* xc, cons
     // a CTA that has its SM to itself, and more steps than the shorter ring holds, gets all of the shared memory (4096 x 4096, 128 tokens:
     // three stages 8.3 us, six 6.3; 11133 x 2976, 77 tokens, 12.0 and 9.9)
     const uint32_t alone = p.split == 8 ? sms - sms / 4 : p.split == 4 ? most : sms;
-    p.stages = std::min(grid <= alone && (p.steps + p.split - 1) / p.split > G::STAGES ? G::STAGES_ALONE : G::STAGES, kMxStages);
+    p.stages = grid <= alone && (p.steps + p.split - 1) / p.split > G::STAGES ? G::STAGES_ALONE : G::STAGES;
     const auto fn = fq_mx_gemm_kernel<T, NT, NV>;
     const uint32_t smem = p.stages * G::STAGE + 1024;
-    const cudaError_t e = ensure_smem_attr((const void*)fn, (int)(std::min(G::STAGES_ALONE, kMxStages) * G::STAGE + 1024));
+    const cudaError_t e = ensure_smem_attr((const void*)fn, (int)(G::STAGES_ALONE * G::STAGE + 1024));
     if (e != cudaSuccess) return fail(FQ_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
     return launch(fn, dim3(grid), G::THREADS, smem, p.split, stream, mw, mx, mws, mxs, p);
 }
@@ -632,7 +630,7 @@ static fq_status_t launch_mx_pair(const fq_mx_layout_t* LX, const void* xc, cons
     if (tiles > 0x7fffffffull) return fail(FQ_ERR_UNSUPPORTED_SHAPE, "too many tiles");
     p.tiles = (uint32_t)tiles;
     p.steps = (p.K + kMxStageK - 1) / kMxStageK;
-    p.stages = G::STAGES < 8 ? G::STAGES : 8;
+    p.stages = G::STAGES;
     const auto fn = fq_mx_pair_kernel<T, NV>;
     const uint32_t smem = p.stages * G::STAGE + 1024;
     const cudaError_t e = ensure_smem_attr((const void*)fn, (int)smem);

@@ -175,7 +175,7 @@ struct MxArgs {
                 return false;
             }
             if (cols > 1 && t.stride(1) != 1) return no(name, "expected adjacent columns");
-            *ld = single ? (one_row ? 0 : cols) : (t.size(0) == 1 ? cols : (uint64_t)t.stride(0));
+            *ld = single ? 0 : t.size(0) == 1 ? cols : (uint64_t)t.stride(0);
             *p = pointer(t, written);
             return true;
         });
