@@ -361,7 +361,7 @@ fq_status_t fq_fused_host_io_async(const fq_layout_t* L, const void* X_host, uin
  *   scales   atoms of 512 bytes, each 128 rows by 4 blocks: the scale of row r and block b is byte
  *                (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4
  *            of atom (r / 128) * ceil(blocks / 4) + b / 4.  Blocks beyond K inside the last atom of a row are 0; bytes of rows
- *            beyond the last are neither read nor written.
+ *            beyond the last are not written, and whatever they hold goes into no result (the product copies whole atoms).
  * (The scales are then in the order in which they go to tensor memory: an atom is one 32x128b copy.)
  *
  * All calls take any number of rows from 1, enqueue on the stream and return.  Unlike the weights of the fused INT4 call,
@@ -414,7 +414,7 @@ fq_status_t fq_mx_dequantize(const fq_mx_layout_t* L, const void* codes, const v
  *     y = block * rsqrt(mean(block^2) + eps) * block_weight  (with it)
  *     r = X + residual_scale * gate * y                      (r = X without block; gate 1 without gate)
  *     h = r * rsqrt(mean(r^2) + eps) * weight                (weight 1 without weight)
- * All of it in binary64 (eps and residual_scale are the given binary32 numbers); r and h are each rounded at the end, by way of binary32, h
+ * All of it as in binary64 (eps and residual_scale are the given binary32 numbers); r and h are each rounded at the end, by way of binary32, h
  * computed from the unrounded r; codes and scales are those that fq_mx_quantize makes of the rounded h.
  * Any of R, H and (codes, scales) may be null, not all.  All of `type`, FQ_TYPE_BF16 or FQ_TYPE_FP16; vectors of D on any
  * boundary; D from 1 to FQ_NORM_MAX_D; with codes, layout.rows = rows and layout.K = D.
@@ -445,7 +445,9 @@ fq_status_t fq_norm_block(const fq_norm_args_t* a, void* cuda_stream);
 /*
  * Product of two quantised matrices, Y[m, n] = ts_x ts_w sum_k x[m, k] w[n, k]: x has LX->rows rows (tokens), w LW->rows
  * rows (output features, K contiguous: a linear layer's weight as it is usually kept).  Same K and format.  Sums in FP32
- * on the tensor cores (tcgen05.mma block_scale), one rounding to `type`.  Y: device, row stride ldy >= LW->rows.
+ * on the tensor cores (tcgen05.mma block_scale).  FQ_MXFP4: the sum is rounded to `type`.  FQ_NVFP4: ts_x ts_w, its product with the sum, and
+ * the rounding to `type` are each rounded, the first two in binary32 (exact where the tensor scales are powers of two).  Y: device, row
+ * stride ldy >= LW->rows.
  * A split along K is added in a fixed order, so results are run-to-run reproducible.  workspace: FQ_MX_WORKSPACE_BYTES of
  * device memory, zeroed once, for fq_check_status; calls may share it.
  */

@@ -14,8 +14,8 @@
 // Few tokens are bound by reading the weights once, and by latency on small layers: the k-steps of a tile are then split
 // over a cluster of CTAs, whose sums meet in shared memory and are added in rank order by all of them, each its tokens.
 // Tensor memory is given back before a CTA waits for its cluster, so that no CTA holds it while it waits for another one.
-// Measured (us, calls back to back in a graph, weights from DRAM): one token 4096 x 4096 4.5, 4096 x 28672 12.2 (5.1 TB/s), 14336 x 4096 NVFP4 8.5
-// (3.9); 128 tokens 5.8, 13.9, 11.9; 128 tokens 8192 x 57344 47 (5.7 TB/s, tensor pipe 35 % busy).  What bounds the small ones is the chain launch,
+// Measured (us, calls back to back in a graph, weights from DRAM): one token 4096 x 4096 4.5, 4096 x 28672 12.0 (5.2 TB/s), 14336 x 4096 NVFP4 8.5
+// (3.9); 128 tokens 5.9, 13.8, 12.0; 128 tokens 8192 x 57344 46 (5.7 TB/s, tensor pipe 35 % busy).  What bounds the small ones is the chain launch,
 // first copy, seven or fewer steps, tensor memory to registers, exchange, store: 3.7 us for 8 steps of 64 tiles.
 #pragma once
 #include <cooperative_groups.h>
@@ -345,10 +345,10 @@ fq_mx_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
 // sums into registers, all at once, give the columns back, and convert and store while the next tile is multiplied.
 // Tiles begin on multiples of 128 tokens, as the atoms of scales do; the last tile of a column multiplies only the tokens that it has,
 // rounded up to 32.
-// What bounds it: of the 12500 clocks of a tile of 4096 k the MMAs need 8200 (tensor pipe 68 % busy); 1700 pass between a tile's last
+// What bounds it: of the 12500 clocks of a tile of 4096 k the MMAs need 8200 (tensor pipe 68 % busy, 83 at the first launch on a cool device); 1700 pass between a tile's last
 // MMA and the next one's first (commit, tensor memory to registers, arrival from the other CTA), the rest waits for copies: six
-// stages of 35 KB are all the shared memory, and the L2 delivers 13 TB/s.  4096 x 4096 x 28672 164 us for the first milliseconds (5.9 PFLOP/s),
-// 197 to 220 once the power cap has lowered the clock to 1.6 GHz; 1024 x 4096 x 18944 29 (5.4 PFLOP/s).  Copies of the next tile's weights to the L2 ahead of time changed nothing.
+// stages of 35 KB are all the shared memory, and the L2 delivers 13 TB/s.  4096 x 4096 x 28672 165 us for the first milliseconds (5.8 PFLOP/s; NVFP4 173),
+// 197 to 220 once the power cap has lowered the clock to 1.6 GHz; 1024 x 4096 x 18944 30 (5.3 PFLOP/s; NVFP4 31).  Copies of the next tile's weights to the L2 ahead of time changed nothing.
 constexpr uint32_t kPairWarps = 12;        // copies, MMAs, allocation, one idle; eight drain warps: two for each 32 features
 
 struct MxPairParams {

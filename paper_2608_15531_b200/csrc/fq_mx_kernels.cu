@@ -21,6 +21,8 @@
 
 namespace fq {
 
+static_assert(FQ_MX_WORKSPACE_BYTES == kWsHeaderBytes + kWsCounterBytes, "fq_check_status clears that much");
+
 __device__ __forceinline__ void grid_start() {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -30,11 +32,14 @@ __device__ __forceinline__ void grid_start() {
 
 // A warp takes 512 consecutive values, 16 to a lane (32 bytes of a 16-bit type: one load), of G rows that are 32 apart.  With
 // G = 4 their scales share the 16-byte lines of an atom, and four loads are in flight; with G = 1 a small matrix is spread over
-// more warps, and gated products, which are bound by instructions, keep to 64 registers.  16 values are a block of FQ_NVFP4, whose scale (a quotient and its rounding) is then
-// computed by one lane.
-// Measured (28672 x 4096 of BF16): MXFP4 45.6 us (6.5 TB/s, the rate of a copy), reading back 46.4; NVFP4 56.3 (5.3 TB/s: 11.8 instructions a
-// value, each rounded twice to see whether the quotient is near a border, 65 % of the issue slots).  Gated products, 4096 x 14336: 64.4 us (MXFP4, BF16;
-// under 30 instructions a value, 72 % of the issue slots, and two of them on the quarter-rate pipe) and 87 (NVFP4, FP16; about 40).
+// more warps, and gated products, which are bound by instructions, keep to 64 registers (those of BF16 spill 8 and 20 bytes for it).  16 values are a
+// block of FQ_NVFP4, whose scale (a quotient and its rounding) is then computed by one lane.
+// Measured (28672 x 4096 of BF16): MXFP4 45.5 us (6.5 TB/s, the rate of a copy), reading back 46.2; NVFP4 55.9 (5.3 TB/s: 11.7 instructions a
+// value, each rounded twice to see whether the quotient is near a border, 69 % of the issue slots).  That is with a tensor scale that no ratio of
+// short numbers is.  With other ones quotients lie on borders all the time, as values of eight bits over scales of four do, and nearly every warp settles some one by
+// one: with 1 BF16 takes 129 us and FP16 75.  FP32: 76.4 and 85.3.  Gated products, 4096 x 14336: 64.3 us (MXFP4, BF16;
+// 28 instructions a value, 72 % of the issue slots, and two of them on the quarter-rate pipe) and 82 to 87 (NVFP4, FP16; about 40; with a tensor scale
+// of 1 95, BF16 111).
 struct MxParams {
     const void* a;               // X, or the gate
     const void* b;               // up
@@ -280,10 +285,11 @@ constexpr int norm_ctas(int tpr, int v) { return v == 1 || tpr >= 768 ? 1 : 768 
 // Sums and results run in binary64.  In binary32 a value of H would cross a border of its type in 1 of 10^4 cases, and a code of every tenth
 // million be a step off.  Only a gate and a weight are multiplied in binary32, exactly (8 + 8 or 11 + 11 bits), as long as the product is a normal number
 // of it.  FP16 products always are; of BF16 a thread looks at its eight, and takes gate and weight one after the other where one is not (or is 0).
-// Norm and gate, 4096 rows of 4096: BF16 49.2 us, FP16 47.7; one after the other throughout 50.8.  What bounds it: 60 instructions
-// a value, half of them the sums over a row and what else a thread does once a row, on 59 % of the issue slots at three rows to an SM (80
+// Norm and gate, 4096 rows of 4096: BF16 49.2 us, FP16 47.7; one after the other throughout 50.8.  What bounds it: 62 instructions
+// a value, half of them the sums over a row and what else a thread does once a row, on 61 % of the issue slots at three rows to an SM (80
 // registers); six conversions a value from and to binary64 keep their pipe 50 % busy.  4096 rows of 4096, with a norm behind the block, a gate
-// and everything put out 49 us (3.6 TB/s), without norm and gate 37; 2048 rows of 16384 103.
+// and everything put out 49 us (3.6 TB/s), without norm and gate 37; R and H alone 44 and 32.  Rows of more than 4096 columns have an SM to themselves,
+// and above 8192 columns 64 registers are too few (52 to 200 bytes spilled): 4096 rows of 5120 104 and 74 us, of 8192 113 and 81; 2048 of 16384 118 and 83.
 template <class T, int TPR, int V, int FORMAT>                             // FORMAT: FQ_MXFP4, FQ_NVFP4, or 2 for none
 __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_ctas(TPR, V)) fq_norm_kernel(const NormParams p) {
     extern __shared__ uint4 ahead[];                       // [2][V][3][threads]: this and the next row's X, block and gate
@@ -481,9 +487,9 @@ static MxParams mx_params(const fq_mx_layout_t* L, const float* ts) {
     return p;
 }
 typedef void (*MxFn)(const MxParams);
-// Rows that a warp takes: four for large matrices (28672 x 4096 of BF16, MXFP4, us, one / four 51.3 / 45.4, NVFP4 93 / 76, read back 48.8 /
-// 46.4; 8192 x 4096 16.0 / 15.9, 28.3 / 25.9, 13.1 / 11.8), one for others, whose time is that of a warp (4096 x 4096 8.7 / 9.7, 15.3 / 15.9, 6.7 / 7.0;
-// 1024 x 4096 2.7 / 3.8, 4.8 / 7.7, 2.6 / 4.0).
+// Rows that a warp takes: four for large matrices (28672 x 4096 of BF16, MXFP4, us, one / four 51.0 / 45.3, NVFP4 74.2 / 55.9, read back 48.6 /
+// 46.1; 8192 x 4096 15.9 / 15.8, 22.6 / 19.3, 14.9 / 13.4), one for others, whose time is that of a warp (4096 x 4096 8.9 / 9.7, 12.4 / 12.0, 8.2 / 7.7;
+// 1024 x 4096 2.9 / 3.4, 3.9 / 4.9, 3.1 / 3.2).
 static bool one_row_tasks(const MxParams& p) { return (uint64_t)p.rows * p.chunks <= 256ull * p.sms; }
 template <class T, bool GATED>
 static MxFn pick_quantize(bool nv, bool one) {
@@ -500,7 +506,7 @@ static MxFn pick_dequantize(bool nv, bool one) {
 static fq_status_t launch_mx(MxFn fn, MxParams& p, uint32_t G, void* stream) {
     // lines of tasks: the first 32 rows of each 32 G (rows 32 further on go with them)
     p.tasks = ((uint64_t)(p.rows / (32 * G)) * 32 + std::min<uint32_t>(p.rows % (32 * G), 32)) * p.chunks;
-    // few warps in CTAs of two, so that they are spread over the SMs (MXFP4, us, two / eight warps: 256 x 4096 1.6 / 1.8, 512 x 4096 2.6 / 2.2)
+    // few warps in CTAs of two, so that they are spread over the SMs (MXFP4, us, two / eight warps: 256 x 4096 1.7 / 1.8, 512 x 4096 2.7 / 2.3)
     const uint32_t threads = p.tasks <= 16ull * p.sms ? 64 : kMxThreads;
     const uint64_t warps = threads / 32, ctas = (p.tasks + warps - 1) / warps;
     if (ctas > 0x7fffffffull) return fail(FQ_ERR_UNSUPPORTED_SHAPE, "matrix too large for one launch");
@@ -509,7 +515,7 @@ static fq_status_t launch_mx(MxFn fn, MxParams& p, uint32_t G, void* stream) {
 
 typedef void (*NormFn)(const NormParams);
 // `tpr`: threads to a row, `v`: vectors of eight to a thread.  Two, which halves what a thread spends on the sums over the row (4096 rows
-// of 4096 49 us, with one 61); but one where every row has an SM to itself and only latency counts.
+// of 4096 49 us, with one 66); but one where every row has an SM to itself and only latency counts.
 template <class T, int FORMAT>
 static NormFn pick_norm(uint32_t D, bool few, uint32_t& tpr, uint32_t& v) {
     const uint32_t vectors = (D + 7) / 8;
@@ -589,10 +595,10 @@ static fq_status_t launch_mx_gemm(const fq_mx_layout_t* LX, const void* xc, cons
     // The steps of a tile over up to eight CTAs.  The first halving costs an exchange of about a microsecond (more tokens: two), each
     // halving saves 0.18 us for each step of a CTA that it takes away, and CTAs that share an SM, or wait for one, lose it again.
     // So: from 16 steps (more than 32 tokens: 32) while a CTA has 8 (16), on as many CTAs as there are SMs, or twice that where the tile is
-    // already split.  us for 1, 2, 4, 8 CTAs: 8 steps, 64 tiles, one token 4.2, 4.7, 4.8, 9.4; 16 steps, 32 tiles 6.2, 5.5, 4.75, 5.1, 64 tokens
-    // 6.0, 6.4, 7.0, 8.2; 56 steps, 32 tiles 14.3, 10.5, 9.4, 8.8, 64 tokens 14.7, 11.4, 10.7, 12.0; 12 steps, 87 tiles 6.8, 7.8, 11, 16.
-    // Clusters of four and eight do not fill every group of SMs: an eighth is left out of the count (34 tiles of eight CTAs, two to
-    // an SM, 10.1 us, of four 6.6; 36 tiles of four with an SM to each 10 us, 33 of them 6.6).
+    // already split.  us for 1, 2, 4, 8 CTAs: 8 steps, 64 tiles, one token 3.7, 4.4, 4.5, 9.0; 16 steps, 32 tiles 5.2, 4.8, 4.5, 4.9, 64 tokens
+    // 5.2, 5.9, 6.8, 7.8; 56 steps, 32 tiles 12.0, 9.7, 9.0, 8.5, 64 tokens 12.8, 10.7, 10.2, 11.5; 12 steps, 87 tiles 6.6, 7.7, 11, 15.
+    // Clusters of four and eight do not fill every group of SMs: an eighth is left out of the count (16 steps, 34 tiles of eight CTAs, two to
+    // an SM, 8.1 us, of four 4.5).
     constexpr uint32_t least = NT <= 32 ? 8 : 16;
     const uint32_t most = sms - sms / 8;
     p.split = 1;
@@ -601,7 +607,8 @@ static fq_status_t launch_mx_gemm(const fq_mx_layout_t* LX, const void* xc, cons
         p.split *= 2;
     const uint32_t grid = p.split > 1 ? p.tiles * p.split : std::min(p.tiles, 2 * sms);
     // a CTA that has its SM to itself, and more steps than the shorter ring holds, gets all of the shared memory (4096 x 4096, 128 tokens:
-    // three stages 8.3 us, six 6.3; 11133 x 2976, 77 tokens, 12.0 and 9.9)
+    // three stages 7.8 us, six 5.8; 11133 x 2976, 77 tokens, 12.0 and 9.9), but not where its cluster would then wait for SMs (36 tiles of four CTAs,
+    // 32 steps, one token: 11.6 us, with the shorter ring 7.0)
     const uint32_t alone = p.split == 8 ? sms - sms / 4 : p.split == 4 ? most : sms;
     p.stages = grid <= alone && (p.steps + p.split - 1) / p.split > G::STAGES ? G::STAGES_ALONE : G::STAGES;
     const auto fn = fq_mx_gemm_kernel<T, NT, NV>;
@@ -638,8 +645,8 @@ static fq_status_t launch_mx_pair(const fq_mx_layout_t* LX, const void* xc, cons
     return launch(fn, dim3(2 * std::min(p.tiles, sms / 2)), 32 * kPairWarps, smem, 1, stream, mw, mx, mws, mxs, p);
 }
 // Tokens of a tile of the pair kernel, 128 or 256: what leaves the busiest pair the fewest bytes to copy, which is what its time goes by (a step's
-// codes and scales of 256 features, and of the tokens that a tile has).  us, 128 / 256: 129 x 4096 x 19200 12.6 / 10.7, 200 x 4096 x 28672 18.0 /
-// 13.8, 2048 x 4096 x 4096 16.5 / 15.0, 640 x 4096 x 28672 44.3 / 38.9; 1024 x 4096 x 6144, the other way, 13.7 / 14.4.
+// codes and scales of 256 features, and of the tokens that a tile has).  us, tiles of 128 / 256, tokens x K x features: 129 x 4096 x 19200 15.0 / 14.1,
+// 200 x 4096 x 28672 19.9 / 16.4, 2048 x 4096 x 4096 17.9 / 15.4, 640 x 4096 x 28672 37.4 / 32.9; 1024 x 4096 x 6144, the other way, 14.4 / 14.7.
 static uint32_t pair_tokens(uint32_t M, uint32_t N, uint32_t sms) {
     auto work = [&](uint32_t t) {
         const uint64_t tiles_m = (M + t - 1) / t, tiles = tiles_m * ((N + 255) / 256), pairs = sms / 2;
@@ -653,8 +660,8 @@ static fq_status_t launch_mx_gemm(const fq_mx_layout_t* LX, const void* xc, cons
     if (p.M <= 16) return launch_mx_gemm<T, 16, NV>(LX, xc, xs, LW, wc, ws, p, sms, stream);
     if (p.M <= 32) return launch_mx_gemm<T, 32, NV>(LX, xc, xs, LW, wc, ws, p, sms, stream);
     if (p.M <= 64) return launch_mx_gemm<T, 64, NV>(LX, xc, xs, LW, wc, ws, p, sms, stream);
-    // More than 128 tokens: single CTAs while each of their tiles has an SM (4096 x 4096, 512 tokens, 128 tiles, 6.6 us, pairs 7.5; 14336 x 4096,
-    // 256 tokens, 13.8 and 17.4), pairs beyond (4096 x 4096, 2048 tokens, 17.0 and 14.6; 4096 x 14336 58 and 42).
+    // More than 128 tokens: single CTAs while each of their tiles has an SM (K 4096, 4096 features, 512 tokens, 128 tiles, 6.8 us, pairs 7.7; K 14336, 4096
+    // features, 256 tokens, 13.2 and 15.3), pairs beyond (K 4096, 4096 features, 2048 tokens, 17.7 and 15.4; K 14336 51 and 41).
     if (p.M > 128 && (uint64_t)((p.M + 127) / 128) * ((p.N + 127) / 128) > sms && sms >= 2)
         return launch_mx_pair<T, NV>(LX, xc, xs, LW, wc, ws, p, pair_tokens(p.M, p.N, sms), sms, stream);
     return launch_mx_gemm<T, 128, NV>(LX, xc, xs, LW, wc, ws, p, sms, stream);
