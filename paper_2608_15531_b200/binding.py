@@ -274,7 +274,7 @@ def fq_check_status(workspace, stream=None) -> None:
     """Waits for the stream (None: the current stream of the workspace's device) and raises what a call on this workspace reported."""
     import torch
     p = _dp(workspace)
-    with torch.cuda.device(workspace.device):
+    with torch.cuda.device(None if workspace is None else workspace.device):
         _check(lib().fq_check_status(p, _stream(stream)))
 
 

@@ -55,3 +55,9 @@ def test_the_status_is_read_behind_the_calls_of_the_scratch_s_own_device(monkeyp
     fq.fq_check_status(Scratch(1), stream=types.SimpleNamespace(cuda_stream=0x77))
     assert cuda.read == [(0x1000, 0x50, 0), (0x2000, 0x51, 1), (0x2000, 0x77, 1)]
     assert cuda.now == 0
+
+
+def test_no_workspace_is_the_library_s_to_refuse(monkeypatch):
+    cuda = Cuda(monkeypatch)
+    fq.fq_check_status(None)
+    assert cuda.read == [(None, 0x50, 0)]
